@@ -14,8 +14,8 @@
  *  - The caller owns every buffer. Buffers of one call do not overlap, but an
  *    output may take the place of an input that it matches element by element
  *    (assigned_rank over topk_idx, pos over assigned_rank, node_pos over
- *    assigned_rank where N = K), and the y of cobalt_node_combine may lie in
- *    expert_out. The four path calls (cobalt_coact_stats,
+ *    assigned_rank where N = K), the y of cobalt_node_combine may lie in
+ *    expert_out, and the experts' calls name theirs. The four path calls (cobalt_coact_stats,
  *    cobalt_assign, cobalt_dispatch_pack, cobalt_combine) allocate nothing,
  *    enqueue their kernels on `stream` (a hipStream_t; NULL = the default
  *    stream of the current device) and return without synchronising.
@@ -286,6 +286,169 @@ cobalt_status cobalt_node_combine(const void* expert_out, const int32_t* pos,
                                   const int32_t* node_pos, int64_t T, int32_t K, int32_t N,
                                   int32_t gpus_per_node, int64_t d, void* node_partial, void* y,
                                   void* stream);
+
+/* ------------------------------------------------------------------------
+ * Gradients of the combine (Step 4): what the experts' outputs and the gates
+ * get from the gradient dy of y.
+ *
+ *   dexpert_out[pos[t][j]][c] = bf16_rne( gates[t][j] * dy[t][c] )
+ *   dgates[t][j] = sum_c dy[t][c] * expert_out[pos[t][j]][c]   (fp32)
+ *
+ * dy [T][d] bf16 in; expert_out [T*K][d] bf16 in (may be NULL without
+ * dgates); pos [T][K] int32 in; gates [T][K] fp32 in (may be NULL without
+ * dexpert_out); dexpert_out [T*K][d] bf16 out (may be NULL): only the rows
+ * that pos names are written, and no two pairs may name one row; dgates
+ * [T][K] fp32 out (may be NULL). A pos outside [0, T*K) writes no row and
+ * has the gate gradient 0. dexpert_out may take the place of expert_out.
+ * The gradient of the dispatch is a combine: cobalt_combine of the rows'
+ * gradients with all gates 1.
+ * ---------------------------------------------------------------------- */
+cobalt_status cobalt_combine_backward(const void* dy, const void* expert_out, const int32_t* pos,
+                                      const float* gates, int64_t T, int32_t K, int64_t d,
+                                      void* dexpert_out, float* dgates, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Pairs grouped by expert: the order in which the experts' products take
+ * their rows.
+ *
+ * topk_idx [T][K] int32 in; pos [T][K] int32 in (from cobalt_dispatch_pack),
+ *   or NULL = pos[p] = p.
+ * With the pairs sorted by (expert, p), place i holding pair p:
+ * rows [T*K] int32 out: pos[p]. tokens [T*K] int32 out (may be NULL): p / K.
+ * expert_offsets [E+1] int32 out: first place of each expert;
+ *   expert_offsets[E] = number of pairs placed.
+ * Pairs with an expert outside [0, E) (tasks that were dropped) are not
+ * placed; rows and tokens are -1 from expert_offsets[E] on.
+ * T = 0 writes expert_offsets alone.
+ * workspace: device scratch of at least
+ *   cobalt_expert_group_workspace_bytes(T, K, E) bytes, 256-byte aligned,
+ *   owned by the caller; contents on entry are ignored; it must not be
+ *   shared by calls that may overlap. The size does not fall as T, K or E
+ *   grows.
+ * ---------------------------------------------------------------------- */
+size_t cobalt_expert_group_workspace_bytes(int64_t T, int32_t K, int32_t E);
+
+cobalt_status cobalt_expert_group(const int32_t* topk_idx, const int32_t* pos, int64_t T,
+                                  int32_t K, int32_t E, int32_t* rows, int32_t* tokens,
+                                  int32_t* expert_offsets, void* workspace,
+                                  size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * The experts: gated feed-forward blocks over rows grouped by expert.
+ *
+ * Common arguments. M: capacity in places; expert_offsets [E+1] int32 in
+ * (from cobalt_expert_group): places [expert_offsets[e], expert_offsets[e+1])
+ * belong to expert e, and places from expert_offsets[E] on are neither read
+ * nor written. rows [M] int32 in, or NULL = rows[i] = i: the row of a
+ * place in a buffer of x_rows (or out_rows) rows. A row outside that buffer
+ * is read as zeros and not written. Offsets outside [0, M] are taken as the
+ * nearest bound; with decreasing ones results are unspecified.
+ * d and f are multiples of 8, at most 2^20; M < 2^31.
+ * Products accumulate in fp32; every bf16 output is rounded once, to
+ * nearest even, from fp32.
+ * act: COBALT_ACT_SILU a(g) = g / (1 + exp(-g)), or COBALT_ACT_GELU
+ * a(g) = g/2 (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))).
+ * ---------------------------------------------------------------------- */
+#define COBALT_ACT_SILU 0
+#define COBALT_ACT_GELU 1
+
+/* Both projections, the activation and the product:
+ *   g[i] = w_in[e][0..f) x[rows[i]],  u[i] = w_in[e][f..2f) x[rows[i]],
+ *   h[i] = bf16_rne( a(g[i]) * u[i] ).
+ * x [x_rows][d] bf16 in; w_in [E][2f][d] bf16 in (gate rows, then up rows);
+ * h [M][f] bf16 out; gate_up [M][2f] bf16 out (may be NULL): g and u, which
+ * the backward pass takes. */
+cobalt_status cobalt_expert_gate_up(const void* x, int64_t x_rows, const int32_t* rows,
+                                    const int32_t* expert_offsets, int64_t M, int32_t E,
+                                    int64_t d, int64_t f, const void* w_in, int32_t act, void* h,
+                                    void* gate_up, void* stream);
+
+/* The output projection: out[rows[i]] = bf16_rne( w_down[e] h[i] ).
+ * h [M][f] bf16 in; w_down [E][d][f] bf16 in; out [out_rows][d] bf16 out:
+ * only rows that a place names are written, and no two places may name one
+ * row. */
+cobalt_status cobalt_expert_down(const void* h, const int32_t* expert_offsets, int64_t M,
+                                 int32_t E, int64_t d, int64_t f, const void* w_down,
+                                 const int32_t* rows, int64_t out_rows, void* out, void* stream);
+
+/* Weight gradients are bf16, or fp32 with COBALT_GRAD_FLOAT; with
+ * COBALT_GRAD_ADD (fp32 only) they are added to what the buffer holds. */
+#define COBALT_GRAD_FLOAT 1
+#define COBALT_GRAD_ADD 2
+
+/* Workspace of the two calls below (partial weight gradients of experts
+ * whose rows are split), 256-byte aligned, owned by the caller, contents
+ * ignored, not shared by calls that may overlap. */
+size_t cobalt_expert_backward_workspace_bytes(int64_t M, int32_t E, int64_t d, int64_t f);
+
+/* Gradients of the output projection, the product and the activation. With
+ * dh[i] = w_down[e]^T dout[rows[i]] in fp32, and g, u from gate_up:
+ *   dgate_up[i] = bf16_rne( dh[i] * u * a'(g) ), bf16_rne( dh[i] * a(g) )
+ *   dw_down[e] (+)= sum_{i of e} dout[rows[i]] h[i]^T.
+ * dout [out_rows][d] bf16 in; gate_up [M][2f], h [M][f] bf16 in (of the
+ * forward calls; h may be NULL without dw_down); dgate_up [M][2f] bf16 out
+ * (may be NULL); dw_down [E][d][f] out (may be NULL), zero for an expert
+ * without places. dgate_up may take the place of gate_up. */
+cobalt_status cobalt_expert_down_backward(const void* dout, int64_t out_rows, const int32_t* rows,
+                                          const int32_t* expert_offsets, int64_t M, int32_t E,
+                                          int64_t d, int64_t f, const void* w_down,
+                                          const void* gate_up, const void* h, int32_t act,
+                                          void* dgate_up, void* dw_down, int32_t flags,
+                                          void* workspace, size_t workspace_bytes, void* stream);
+
+/* Gradients of the two projections:
+ *   dx[rows[i]] = bf16_rne( w_in[e]^T dgate_up[i] )
+ *   dw_in[e] (+)= sum_{i of e} dgate_up[i] x[rows[i]]^T.
+ * dgate_up [M][2f] bf16 in; x [x_rows][d] bf16 in (may be NULL without
+ * dw_in); w_in [E][2f][d] bf16 in; dx [x_rows][d] bf16 out (may be NULL):
+ * only rows that a place names are written, and no two places may name one
+ * row; dw_in [E][2f][d] out (may be NULL), zero for an expert without
+ * places. dx and x must not overlap unless dw_in is NULL. */
+cobalt_status cobalt_expert_gate_up_backward(const void* dgate_up, const void* x, int64_t x_rows,
+                                             const int32_t* rows, const int32_t* expert_offsets,
+                                             int64_t M, int32_t E, int64_t d, int64_t f,
+                                             const void* w_in, void* dx, void* dw_in,
+                                             int32_t flags, void* workspace,
+                                             size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Microscaled 4-bit rows (MXFP4 of the OCP Microscaling Formats
+ * specification 1.0): blocks of 32 values along a row share a scale.
+ *
+ * A row of n values (n a multiple of 32) is n/2 bytes of E2M1 codes, two to
+ * a byte, the lower-numbered value in the low half, and n/32 bytes of E8M0
+ * scales, byte b standing for 2^(b-127). E2M1 has sign bit 8 and the values
+ * 0, 0.5, 1, 1.5, 2, 3, 4, 6.
+ * cobalt_mx_quantize: with m the largest magnitude of a block, the scale is
+ *   2^max(floor(log2 m) - 2, -127) (2^-127 for m = 0), and each value over
+ *   the scale is rounded to the nearest E2M1 value, ties to the even code,
+ *   magnitudes over 6 to 6. A block that holds an infinity or NaN gets the
+ *   scale byte 255 (NaN) and codes 0.
+ * cobalt_mx_dequantize: the values, exact in bf16; NaN where the scale byte
+ *   is 255.
+ * x, y [R][n] bf16; codes [R][n/2] uint8; scales [R][n/32] uint8; R >= 0,
+ * R * n < 2^47; codes 16-byte aligned.
+ * ---------------------------------------------------------------------- */
+cobalt_status cobalt_mx_quantize(const void* x, int64_t R, int64_t n, void* codes, void* scales,
+                                 void* stream);
+cobalt_status cobalt_mx_dequantize(const void* codes, const void* scales, int64_t R, int64_t n,
+                                   void* y, void* stream);
+
+/* cobalt_expert_gate_up and cobalt_expert_down on microscaled rows and
+ * weights: the same formulas, on the values that codes and scales stand
+ * for, accumulated in fp32. d and f are multiples of 32.
+ * x_codes [x_rows][d/2], x_scales [x_rows][d/32]; w_codes [E][2f][d/2],
+ * w_scales [E][2f][d/32]; h [M][f] bf16 out.
+ * h_codes [M][f/2], h_scales [M][f/32]; w_codes [E][d][f/2], w_scales
+ * [E][d][f/32]; out [out_rows][d] bf16 out. */
+cobalt_status cobalt_mx_gate_up(const void* x_codes, const void* x_scales, int64_t x_rows,
+                                const int32_t* rows, const int32_t* expert_offsets, int64_t M,
+                                int32_t E, int64_t d, int64_t f, const void* w_codes,
+                                const void* w_scales, int32_t act, void* h, void* stream);
+cobalt_status cobalt_mx_down(const void* h_codes, const void* h_scales,
+                             const int32_t* expert_offsets, int64_t M, int32_t E, int64_t d,
+                             int64_t f, const void* w_codes, const void* w_scales,
+                             const int32_t* rows, int64_t out_rows, void* out, void* stream);
 
 /* ------------------------------------------------------------------------
  * Per-replica workload (Section 3.1 workload model: w_er counts the tasks of

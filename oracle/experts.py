@@ -1,0 +1,110 @@
+"""Oracle of the experts' operators (test infrastructure only): the formulas
+in numpy, in 64 bits, one expert at a time. Shares no code with the library.
+
+Products come with the sum of the magnitudes of their terms, from which a
+test derives how far an fp32 accumulation may be off.
+"""
+from __future__ import annotations
+
+import numpy as np
+
+SILU, GELU = 0, 1
+E2M1 = np.array([0, 0.5, 1, 1.5, 2, 3, 4, 6, -0.0, -0.5, -1, -1.5, -2, -3, -4, -6])
+
+
+def wide(bits):
+    """bf16 bits (uint16) as float64."""
+    with np.errstate(invalid="ignore"):  # signalling NaN patterns
+        return (np.asarray(bits, np.uint16).astype(np.uint32) << 16).view(np.float32).astype(
+            np.float64)
+
+
+def group(topk, pos, E):
+    """(rows, tokens, offsets): a cursor over the experts, pair by pair."""
+    T, K = topk.shape
+    rows, tokens, offsets = [], [], [0]
+    for e in range(E):
+        for p in np.nonzero(topk.reshape(-1) == e)[0]:
+            rows.append(p if pos is None else pos.reshape(-1)[p])
+            tokens.append(p // K)
+        offsets.append(len(rows))
+    pad = [-1] * (T * K - len(rows))
+    return (np.array(rows + pad, np.int32), np.array(tokens + pad, np.int32),
+            np.array(offsets, np.int32))
+
+
+def act(g, kind):
+    with np.errstate(over="ignore"):
+        if kind == SILU:
+            return g / (1 + np.exp(-g))
+        return g / 2 * (1 + np.tanh(np.sqrt(2 / np.pi) * (g + 0.044715 * g ** 3)))
+
+
+def act_slope(g, kind):
+    with np.errstate(over="ignore"):
+        if kind == SILU:
+            s = 1 / (1 + np.exp(-g))
+            return s + g * s * (1 - s)
+        c = np.sqrt(2 / np.pi)
+        t = np.tanh(c * (g + 0.044715 * g ** 3))
+        return (1 + t) / 2 + g / 2 * (1 - t ** 2) * c * (1 + 3 * 0.044715 * g ** 2)
+
+
+def taken(x, rows, M):
+    """Row rows[i] of x for each place i, zeros where x has no such row."""
+    out = np.zeros((M, x.shape[1]))
+    for i in range(M):
+        r = i if rows is None else rows[i]
+        if 0 <= r < x.shape[0]:
+            out[i] = x[r]
+    return out
+
+
+def per_expert(a, offsets, w):
+    """y[i] = w[e(i)] a[i] and the sums of the terms' magnitudes, for the
+    places that belong to an expert (zeros behind them)."""
+    y, size = np.zeros((2, a.shape[0], w.shape[1]))
+    for e in range(w.shape[0]):
+        s = slice(offsets[e], offsets[e + 1])
+        y[s] = a[s] @ w[e].T
+        size[s] = np.abs(a[s]) @ np.abs(w[e]).T
+    return y, size
+
+
+def outer_sums(a, b, offsets):
+    """sum_{i of e} a[i] b[i]^T of each expert, and of the magnitudes."""
+    E = len(offsets) - 1
+    y, size = np.zeros((2, E, a.shape[1], b.shape[1]))
+    for e in range(E):
+        s = slice(offsets[e], offsets[e + 1])
+        y[e] = a[s].T @ b[s]
+        size[e] = np.abs(a[s]).T @ np.abs(b[s])
+    return y, size
+
+
+def quantize(x):
+    """(codes, scales) of float64 rows, value by value from the definition."""
+    R, n = x.shape
+    codes, scales = np.zeros((R, n // 2), np.uint8), np.zeros((R, n // 32), np.uint8)
+    for r in range(R):
+        for b in range(n // 32):
+            v = x[r, 32 * b:32 * b + 32]
+            if not np.isfinite(v).all():
+                scales[r, b] = 255
+                continue
+            big = np.abs(v).max()
+            ex = -127 if big == 0 else max(int(np.floor(np.log2(big))) - 2, -127)
+            scales[r, b] = ex + 127
+            for i, m in enumerate(np.abs(v) * 2.0 ** -ex):
+                off = np.abs(E2M1[:8] - m)
+                best = [c for c in range(8) if off[c] == off.min()]
+                c = best[0] if len(best) == 1 else [c for c in best if c % 2 == 0][0]
+                c += 8 * int(np.signbit(v[i]))
+                codes[r, (32 * b + i) // 2] |= c << (4 * (i % 2))
+    return codes, scales
+
+
+def dequantize(codes, scales):
+    v = np.stack([E2M1[codes & 15], E2M1[codes >> 4]], -1).reshape(*codes.shape[:-1], -1)
+    s = np.where(scales == 255, np.nan, 2.0 ** (scales.astype(np.float64) - 127))
+    return v * np.repeat(s, 32, -1)

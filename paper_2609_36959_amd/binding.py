@@ -9,6 +9,7 @@ built, every call raises; there is no fallback path.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from typing import Optional
 
@@ -72,6 +73,22 @@ def lib() -> ctypes.CDLL:
         "cobalt_replica_load_workspace_bytes": ([i64, i32, i32, i32], sz),
         "cobalt_replica_load": ([P, P, i64, i32, i32, i32, P, P, sz, P], ctypes.c_int),
         "cobalt_intra_node_rebalance": ([i32, i32, i32, i32, P, P, P, P, P, P], ctypes.c_int),
+        "cobalt_combine_backward": ([P, P, P, P, i64, i32, i64, P, P, P], ctypes.c_int),
+        "cobalt_expert_group_workspace_bytes": ([i64, i32, i32], sz),
+        "cobalt_expert_group": ([P, P, i64, i32, i32, P, P, P, P, sz, P], ctypes.c_int),
+        "cobalt_expert_gate_up": ([P, i64, P, P, i64, i32, i64, i64, P, i32, P, P, P],
+                                  ctypes.c_int),
+        "cobalt_expert_down": ([P, P, i64, i32, i64, i64, P, P, i64, P, P], ctypes.c_int),
+        "cobalt_expert_backward_workspace_bytes": ([i64, i32, i64, i64], sz),
+        "cobalt_expert_down_backward": ([P, i64, P, P, i64, i32, i64, i64, P, P, P, i32, P, P,
+                                         i32, P, sz, P], ctypes.c_int),
+        "cobalt_expert_gate_up_backward": ([P, P, i64, P, P, i64, i32, i64, i64, P, P, P, i32, P,
+                                            sz, P], ctypes.c_int),
+        "cobalt_mx_quantize": ([P, i64, i64, P, P, P], ctypes.c_int),
+        "cobalt_mx_dequantize": ([P, P, i64, i64, P, P], ctypes.c_int),
+        "cobalt_mx_gate_up": ([P, P, i64, P, P, i64, i32, i64, i64, P, P, i32, P, P],
+                              ctypes.c_int),
+        "cobalt_mx_down": ([P, P, P, i64, i32, i64, i64, P, P, P, i64, P, P], ctypes.c_int),
         "cobalt_plan_layout": ([i32, i32, i32, i32, P, P, ctypes.c_float, P, P, P, P, P],
                                ctypes.c_int),
     }
@@ -124,6 +141,7 @@ U16 = (torch.int16, torch.uint16)
 BF16 = (torch.bfloat16,)
 F32 = (torch.float32,)
 I64 = (torch.int64,)
+U8 = (torch.uint8,)
 WS = (torch.uint8, torch.int8, torch.int32, torch.int64)
 
 
@@ -306,6 +324,164 @@ def cobalt_node_combine(expert_out: torch.Tensor, pos: torch.Tensor, assigned_ra
           _dev(gates, "gates", F32, (T, K)), _dev(node_pos, "node_pos", I32, (T, N)), T, K, N,
           gpus_per_node, d, _dev(node_partial, "node_partial", BF16, (T * min(K, N), d)),
           _dev(y, "y", BF16, (T, d)), _stream(stream))
+
+
+# ------------------------------------------------------------------- experts
+ACT_SILU, ACT_GELU = 0, 1
+GRAD_FLOAT, GRAD_ADD = 1, 2
+
+
+def cobalt_combine_backward(dy: torch.Tensor, expert_out: Optional[torch.Tensor],
+                            pos: torch.Tensor, gates: Optional[torch.Tensor],
+                            dexpert_out: Optional[torch.Tensor] = None,
+                            dgates: Optional[torch.Tensor] = None, stream=None) -> None:
+    T, K = pos.shape
+    d = dy.shape[1]
+    _call("cobalt_combine_backward", _dev(dy, "dy", BF16, (T, d)),
+          _dev(expert_out, "expert_out", BF16, (T * K, d)), _dev(pos, "pos", I32),
+          _dev(gates, "gates", F32, (T, K)), T, K, d,
+          _dev(dexpert_out, "dexpert_out", BF16, (T * K, d)),
+          _dev(dgates, "dgates", F32, (T, K)), _stream(stream))
+
+
+def cobalt_expert_group_workspace_bytes(T: int, K: int, E: int) -> int:
+    return int(lib().cobalt_expert_group_workspace_bytes(T, K, E))
+
+
+def cobalt_expert_group(topk_idx: torch.Tensor, pos: Optional[torch.Tensor], E: int,
+                        rows: torch.Tensor, expert_offsets: torch.Tensor,
+                        workspace: torch.Tensor, tokens: Optional[torch.Tensor] = None,
+                        stream=None) -> None:
+    T, K = topk_idx.shape
+    _call("cobalt_expert_group", _dev(topk_idx, "topk_idx", I32), _dev(pos, "pos", I32, (T, K)),
+          T, K, E, _dev(rows, "rows", I32, (T * K,)), _dev(tokens, "tokens", I32, (T * K,)),
+          _dev(expert_offsets, "expert_offsets", I32, (E + 1,)),
+          _dev(workspace, "workspace", WS), workspace.numel() * workspace.element_size(),
+          _stream(stream))
+
+
+def cobalt_expert_gate_up(x: torch.Tensor, rows: Optional[torch.Tensor],
+                          expert_offsets: torch.Tensor, w_in: torch.Tensor, h: torch.Tensor,
+                          gate_up: Optional[torch.Tensor] = None, act: int = ACT_SILU,
+                          stream=None) -> None:
+    """x [x_rows, d], rows [M] or None, w_in [E, 2f, d] -> h [M, f] and, if
+    given, gate_up [M, 2f]."""
+    (M, f), (E, d) = h.shape, (w_in.shape[0], x.shape[1])
+    _call("cobalt_expert_gate_up", _dev(x, "x", BF16), x.shape[0], _dev(rows, "rows", I32, (M,)),
+          _dev(expert_offsets, "expert_offsets", I32, (E + 1,)), M, E, d, f,
+          _dev(w_in, "w_in", BF16, (E, 2 * f, d)), act, _dev(h, "h", BF16),
+          _dev(gate_up, "gate_up", BF16, (M, 2 * f)), _stream(stream))
+
+
+def cobalt_expert_down(h: torch.Tensor, expert_offsets: torch.Tensor, w_down: torch.Tensor,
+                       rows: Optional[torch.Tensor], out: torch.Tensor, stream=None) -> None:
+    """h [M, f], w_down [E, d, f], rows [M] or None -> out [out_rows, d]."""
+    (M, f), (E, d) = h.shape, w_down.shape[:2]
+    _call("cobalt_expert_down", _dev(h, "h", BF16),
+          _dev(expert_offsets, "expert_offsets", I32, (E + 1,)), M, E, d, f,
+          _dev(w_down, "w_down", BF16, (E, d, f)), _dev(rows, "rows", I32, (M,)), out.shape[0],
+          _dev(out, "out", BF16, (out.shape[0], d)), _stream(stream))
+
+
+def cobalt_expert_backward_workspace_bytes(M: int, E: int, d: int, f: int) -> int:
+    return int(lib().cobalt_expert_backward_workspace_bytes(M, E, d, f))
+
+
+def _grad(t: Optional[torch.Tensor], name: str, flags: int, shape) -> Optional[int]:
+    return _dev(t, name, F32 if flags & GRAD_FLOAT else BF16, shape)
+
+
+def cobalt_expert_down_backward(dout: torch.Tensor, rows: Optional[torch.Tensor],
+                                expert_offsets: torch.Tensor, w_down: torch.Tensor,
+                                gate_up: torch.Tensor, h: Optional[torch.Tensor],
+                                dgate_up: Optional[torch.Tensor],
+                                dw_down: Optional[torch.Tensor], workspace: torch.Tensor,
+                                act: int = ACT_SILU, flags: int = 0, stream=None) -> None:
+    """dout [out_rows, d], gate_up [M, 2f], h [M, f] -> dgate_up [M, 2f] and
+    dw_down [E, d, f] (bf16, or fp32 with GRAD_FLOAT)."""
+    M, (E, d, f) = gate_up.shape[0], w_down.shape
+    _call("cobalt_expert_down_backward", _dev(dout, "dout", BF16, (dout.shape[0], d)),
+          dout.shape[0], _dev(rows, "rows", I32, (M,)),
+          _dev(expert_offsets, "expert_offsets", I32, (E + 1,)), M, E, d, f,
+          _dev(w_down, "w_down", BF16), _dev(gate_up, "gate_up", BF16, (M, 2 * f)),
+          _dev(h, "h", BF16, (M, f)), act, _dev(dgate_up, "dgate_up", BF16, (M, 2 * f)),
+          _grad(dw_down, "dw_down", flags, (E, d, f)), flags, _dev(workspace, "workspace", WS),
+          workspace.numel() * workspace.element_size(), _stream(stream))
+
+
+def cobalt_expert_gate_up_backward(dgate_up: torch.Tensor, x: Optional[torch.Tensor],
+                                   rows: Optional[torch.Tensor], expert_offsets: torch.Tensor,
+                                   w_in: torch.Tensor, dx: Optional[torch.Tensor],
+                                   dw_in: Optional[torch.Tensor], workspace: torch.Tensor,
+                                   flags: int = 0, stream=None) -> None:
+    """dgate_up [M, 2f], x [x_rows, d] -> dx [x_rows, d] and dw_in [E, 2f, d]
+    (bf16, or fp32 with GRAD_FLOAT)."""
+    M, (E, f, d) = dgate_up.shape[0], (w_in.shape[0], w_in.shape[1] // 2, w_in.shape[2])
+    n = (x if x is not None else dx).shape[0] if x is not None or dx is not None else M
+    _call("cobalt_expert_gate_up_backward", _dev(dgate_up, "dgate_up", BF16, (M, 2 * f)),
+          _dev(x, "x", BF16, (n, d)), n, _dev(rows, "rows", I32, (M,)),
+          _dev(expert_offsets, "expert_offsets", I32, (E + 1,)), M, E, d, f,
+          _dev(w_in, "w_in", BF16, (E, 2 * f, d)), _dev(dx, "dx", BF16, (n, d)),
+          _grad(dw_in, "dw_in", flags, (E, 2 * f, d)), flags, _dev(workspace, "workspace", WS),
+          workspace.numel() * workspace.element_size(), _stream(stream))
+
+
+def cobalt_mx_quantize(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor,
+                       stream=None) -> None:
+    """x [..., n] bf16 -> codes [..., n / 2], scales [..., n / 32] uint8."""
+    *lead, n = x.shape
+    _call("cobalt_mx_quantize", _dev(x, "x", BF16), math.prod(lead), n,
+          _dev(codes, "codes", U8, (*lead, n // 2)), _dev(scales, "scales", U8, (*lead, n // 32)),
+          _stream(stream))
+
+
+def cobalt_mx_dequantize(codes: torch.Tensor, scales: torch.Tensor, y: torch.Tensor,
+                         stream=None) -> None:
+    *lead, n = y.shape
+    _call("cobalt_mx_dequantize", _dev(codes, "codes", U8, (*lead, n // 2)),
+          _dev(scales, "scales", U8, (*lead, n // 32)), math.prod(lead), n, _dev(y, "y", BF16),
+          _stream(stream))
+
+
+def cobalt_mx_gate_up(x_codes: torch.Tensor, x_scales: torch.Tensor,
+                      rows: Optional[torch.Tensor], expert_offsets: torch.Tensor,
+                      w_codes: torch.Tensor, w_scales: torch.Tensor, h: torch.Tensor,
+                      act: int = ACT_SILU, stream=None) -> None:
+    """cobalt_expert_gate_up on 4-bit rows [x_rows, d] and weights [E, 2f, d]."""
+    (M, f), E, (n, half) = h.shape, w_codes.shape[0], x_codes.shape
+    d = 2 * half
+    _call("cobalt_mx_gate_up", _dev(x_codes, "x_codes", U8),
+          _dev(x_scales, "x_scales", U8, (n, d // 32)), n, _dev(rows, "rows", I32, (M,)),
+          _dev(expert_offsets, "expert_offsets", I32, (E + 1,)), M, E, d, f,
+          _dev(w_codes, "w_codes", U8, (E, 2 * f, half)),
+          _dev(w_scales, "w_scales", U8, (E, 2 * f, d // 32)), act, _dev(h, "h", BF16),
+          _stream(stream))
+
+
+def cobalt_mx_down(h_codes: torch.Tensor, h_scales: torch.Tensor, expert_offsets: torch.Tensor,
+                   w_codes: torch.Tensor, w_scales: torch.Tensor, rows: Optional[torch.Tensor],
+                   out: torch.Tensor, stream=None) -> None:
+    """cobalt_expert_down on 4-bit rows [M, f] and weights [E, d, f]."""
+    (M, half), (E, d) = h_codes.shape, w_codes.shape[:2]
+    f = 2 * half
+    _call("cobalt_mx_down", _dev(h_codes, "h_codes", U8),
+          _dev(h_scales, "h_scales", U8, (M, f // 32)),
+          _dev(expert_offsets, "expert_offsets", I32, (E + 1,)), M, E, d, f,
+          _dev(w_codes, "w_codes", U8, (E, d, half)),
+          _dev(w_scales, "w_scales", U8, (E, d, f // 32)), _dev(rows, "rows", I32, (M,)),
+          out.shape[0], _dev(out, "out", BF16, (out.shape[0], d)), _stream(stream))
+
+
+def expert_group_workspace_for(T: int, K: int, E: int, device="cuda") -> torch.Tensor:
+    """A grouping workspace of the size the library asks for."""
+    n = cobalt_expert_group_workspace_bytes(T, K, E)
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+
+
+def expert_backward_workspace_for(M: int, E: int, d: int, f: int, device="cuda") -> torch.Tensor:
+    """A workspace for the experts' backward calls of the size the library asks for."""
+    n = cobalt_expert_backward_workspace_bytes(M, E, d, f)
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
 
 
 def cobalt_replica_load_workspace_bytes(T: int, K: int, E: int, G: int) -> int:

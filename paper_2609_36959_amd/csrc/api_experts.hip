@@ -1,0 +1,189 @@
+// C entry points of the experts' operators: argument checks and dispatch to
+// the kernel launchers.
+#include "experts.hpp"
+
+using namespace cobalt;
+
+namespace {
+
+constexpr int64_t kMaxWidth = int64_t(1) << 20;
+constexpr int64_t kMaxPlaces = (int64_t(1) << 31) - 1;
+
+bool aligned(const void* p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
+
+// Sizes and index arrays that every product of the experts takes; `unit`
+// divides both widths. Rows without an index are the places themselves.
+cobalt_status check_experts(const int32_t* off, int64_t M, int32_t E, int64_t d, int64_t f,
+                            int64_t unit, const int32_t* rows, int64_t n_rows) {
+    if (M < 0 || E < 1 || E > kMaxE || !off) return COBALT_EINVAL;
+    if (d < unit || f < unit || d % unit != 0 || f % unit != 0) return COBALT_EINVAL;
+    if (n_rows < 0 || (!rows && n_rows < M)) return COBALT_EINVAL;
+    if (M > kMaxPlaces || d > kMaxWidth || f > kMaxWidth) return COBALT_EUNSUPPORTED;
+    return COBALT_OK;
+}
+
+bool act_ok(int32_t act) { return act == COBALT_ACT_SILU || act == COBALT_ACT_GELU; }
+
+bool flags_ok(int32_t flags) {
+    return flags == 0 || flags == COBALT_GRAD_FLOAT ||
+           flags == (COBALT_GRAD_FLOAT | COBALT_GRAD_ADD);
+}
+
+// A buffer that the call needs: there, and aligned for 16-byte accesses.
+bool rows_ok(const void* p) { return p && aligned(p, 16); }
+
+}  // namespace
+
+extern "C" cobalt_status cobalt_combine_backward(const void* dy, const void* eo,
+                                                 const int32_t* pos, const float* gates,
+                                                 int64_t T, int32_t K, int64_t d, void* deo,
+                                                 float* dgates, void* stream) {
+    if (T < 0 || K < 1 || K > kMaxK || d < 8 || d % 8 != 0) return COBALT_EINVAL;
+    if (T > 0 && (!rows_ok(dy) || !pos)) return COBALT_EINVAL;
+    if (T > 0 && ((dgates && !rows_ok(eo)) || (deo && (!gates || !aligned(deo, 16)))))
+        return COBALT_EINVAL;
+    if (T * K >= (int64_t(1) << 31)) return COBALT_EUNSUPPORTED;
+    if (T == 0 || (!deo && !dgates)) return COBALT_OK;
+    return launch_combine_backward(dy, eo, pos, gates, T, K, d, deo, dgates, (hipStream_t)stream);
+}
+
+extern "C" size_t cobalt_expert_group_workspace_bytes(int64_t T, int32_t K, int32_t E) {
+    if (T < 0 || K < 1 || K > kMaxK || E < 1 || E > kMaxE || T * K >= (int64_t(1) << 31)) return 0;
+    return expert_group_workspace_bytes(T, K, E);
+}
+
+extern "C" cobalt_status cobalt_expert_group(const int32_t* topk, const int32_t* pos, int64_t T,
+                                             int32_t K, int32_t E, int32_t* rows, int32_t* tokens,
+                                             int32_t* offsets, void* ws, size_t ws_bytes,
+                                             void* stream) {
+    if (T < 0 || K < 1 || K > kMaxK || E < 1 || E > kMaxE || !offsets || !ws) return COBALT_EINVAL;
+    if (T > 0 && (!topk || !rows)) return COBALT_EINVAL;
+    if (!aligned(ws, 256)) return COBALT_EINVAL;
+    if (T * K >= (int64_t(1) << 31)) return COBALT_EUNSUPPORTED;
+    if (ws_bytes < expert_group_workspace_bytes(T, K, E)) return COBALT_EINVAL;
+    return launch_expert_group(topk, pos, T, K, E, rows, tokens, offsets, ws, (hipStream_t)stream);
+}
+
+extern "C" cobalt_status cobalt_expert_gate_up(const void* x, int64_t x_rows, const int32_t* rows,
+                                               const int32_t* off, int64_t M, int32_t E, int64_t d,
+                                               int64_t f, const void* w_in, int32_t act, void* h,
+                                               void* gate_up, void* stream) {
+    if (cobalt_status st = check_experts(off, M, E, d, f, 8, rows, x_rows)) return st;
+    if (!act_ok(act) || !rows_ok(w_in)) return COBALT_EINVAL;
+    if (M > 0 && ((x_rows > 0 && !rows_ok(x)) || !rows_ok(h) || !aligned(gate_up, 16)))
+        return COBALT_EINVAL;
+    if (M == 0) return COBALT_OK;
+    return launch_gate_up({off, E, (int32_t)M}, x, {rows, x_rows}, d, f, w_in, (Act)act, h,
+                          gate_up, (hipStream_t)stream);
+}
+
+extern "C" cobalt_status cobalt_expert_down(const void* h, const int32_t* off, int64_t M,
+                                            int32_t E, int64_t d, int64_t f, const void* w_down,
+                                            const int32_t* rows, int64_t out_rows, void* out,
+                                            void* stream) {
+    if (cobalt_status st = check_experts(off, M, E, d, f, 8, rows, out_rows)) return st;
+    if (!rows_ok(w_down)) return COBALT_EINVAL;
+    if (M > 0 && (!rows_ok(h) || (out_rows > 0 && !rows_ok(out)))) return COBALT_EINVAL;
+    if (M == 0 || out_rows == 0) return COBALT_OK;
+    return launch_down({off, E, (int32_t)M}, h, d, f, w_down, {rows, out_rows}, out,
+                       (hipStream_t)stream);
+}
+
+extern "C" size_t cobalt_expert_backward_workspace_bytes(int64_t M, int32_t E, int64_t d,
+                                                         int64_t f) {
+    if (M < 0 || M > kMaxPlaces || E < 1 || E > kMaxE || d < 8 || d % 8 != 0 || d > kMaxWidth ||
+        f < 8 || f % 8 != 0 || f > kMaxWidth)
+        return 0;
+    return expert_backward_workspace_bytes(M, E, d, f);
+}
+
+extern "C" cobalt_status cobalt_expert_down_backward(
+    const void* dout, int64_t out_rows, const int32_t* rows, const int32_t* off, int64_t M,
+    int32_t E, int64_t d, int64_t f, const void* w_down, const void* gate_up, const void* h,
+    int32_t act, void* dgate_up, void* dw_down, int32_t flags, void* ws, size_t ws_bytes,
+    void* stream) {
+    if (cobalt_status st = check_experts(off, M, E, d, f, 8, rows, out_rows)) return st;
+    if (!act_ok(act) || !flags_ok(flags) || !ws || !aligned(ws, 256)) return COBALT_EINVAL;
+    if (ws_bytes < expert_backward_workspace_bytes(M, E, d, f)) return COBALT_EINVAL;
+    if (M > 0 && out_rows > 0 && !rows_ok(dout)) return COBALT_EINVAL;
+    if (dgate_up && (!rows_ok(w_down) || (M > 0 && (!rows_ok(gate_up) || !aligned(dgate_up, 16)))))
+        return COBALT_EINVAL;
+    if (dw_down && (!aligned(dw_down, 16) || (M > 0 && !rows_ok(h)))) return COBALT_EINVAL;
+    const Groups g{off, E, (int32_t)M};
+    const Rows at{rows, out_rows};
+    const hipStream_t s = (hipStream_t)stream;
+    if (dw_down)
+        if (cobalt_status st = launch_weight_gradient(g, dout, d, true, h, f, false, at, dw_down,
+                                                      flags & COBALT_GRAD_FLOAT,
+                                                      flags & COBALT_GRAD_ADD, ws, s))
+            return st;
+    if (!dgate_up || M == 0) return COBALT_OK;
+    return launch_down_gradient(g, dout, at, d, f, w_down, gate_up, (Act)act, dgate_up, s);
+}
+
+extern "C" cobalt_status cobalt_expert_gate_up_backward(
+    const void* dgate_up, const void* x, int64_t x_rows, const int32_t* rows, const int32_t* off,
+    int64_t M, int32_t E, int64_t d, int64_t f, const void* w_in, void* dx, void* dw_in,
+    int32_t flags, void* ws, size_t ws_bytes, void* stream) {
+    if (cobalt_status st = check_experts(off, M, E, d, f, 8, rows, x_rows)) return st;
+    if (!flags_ok(flags) || !ws || !aligned(ws, 256)) return COBALT_EINVAL;
+    if (ws_bytes < expert_backward_workspace_bytes(M, E, d, f)) return COBALT_EINVAL;
+    if (M > 0 && !rows_ok(dgate_up)) return COBALT_EINVAL;
+    if (dx && (!rows_ok(w_in) || !aligned(dx, 16))) return COBALT_EINVAL;
+    if (dw_in && (!aligned(dw_in, 16) || (M > 0 && x_rows > 0 && !rows_ok(x))))
+        return COBALT_EINVAL;
+    const Groups g{off, E, (int32_t)M};
+    const Rows at{rows, x_rows};
+    const hipStream_t s = (hipStream_t)stream;
+    if (dw_in)
+        if (cobalt_status st = launch_weight_gradient(g, dgate_up, 2 * f, false, x, d, true, at,
+                                                      dw_in, flags & COBALT_GRAD_FLOAT,
+                                                      flags & COBALT_GRAD_ADD, ws, s))
+            return st;
+    if (!dx || M == 0 || x_rows == 0) return COBALT_OK;
+    return launch_gate_up_gradient(g, dgate_up, d, f, w_in, at, dx, s);
+}
+
+static bool mx_sizes_ok(int64_t R, int64_t n) { return R >= 0 && n >= 32 && n % 32 == 0; }
+
+extern "C" cobalt_status cobalt_mx_quantize(const void* x, int64_t R, int64_t n, void* codes,
+                                            void* scales, void* stream) {
+    if (!mx_sizes_ok(R, n)) return COBALT_EINVAL;
+    if (R > 0 && (!rows_ok(x) || !rows_ok(codes) || !scales)) return COBALT_EINVAL;
+    if (R > 0 && n >= (int64_t(1) << 47) / R) return COBALT_EUNSUPPORTED;
+    if (R == 0) return COBALT_OK;
+    return launch_mx_quantize(x, R, n, codes, scales, (hipStream_t)stream);
+}
+
+extern "C" cobalt_status cobalt_mx_dequantize(const void* codes, const void* scales, int64_t R,
+                                              int64_t n, void* y, void* stream) {
+    if (!mx_sizes_ok(R, n)) return COBALT_EINVAL;
+    if (R > 0 && (!rows_ok(y) || !rows_ok(codes) || !scales)) return COBALT_EINVAL;
+    if (R > 0 && n >= (int64_t(1) << 47) / R) return COBALT_EUNSUPPORTED;
+    if (R == 0) return COBALT_OK;
+    return launch_mx_dequantize(codes, scales, R, n, y, (hipStream_t)stream);
+}
+
+extern "C" cobalt_status cobalt_mx_gate_up(const void* xc, const void* xs, int64_t x_rows,
+                                           const int32_t* rows, const int32_t* off, int64_t M,
+                                           int32_t E, int64_t d, int64_t f, const void* wc,
+                                           const void* ws, int32_t act, void* h, void* stream) {
+    if (cobalt_status st = check_experts(off, M, E, d, f, 32, rows, x_rows)) return st;
+    if (!act_ok(act) || !rows_ok(wc) || !ws) return COBALT_EINVAL;
+    if (M > 0 && ((x_rows > 0 && (!rows_ok(xc) || !xs)) || !rows_ok(h))) return COBALT_EINVAL;
+    if (M == 0) return COBALT_OK;
+    return launch_mx_gate_up({off, E, (int32_t)M}, xc, xs, {rows, x_rows}, d, f, wc, ws, (Act)act,
+                             h, (hipStream_t)stream);
+}
+
+extern "C" cobalt_status cobalt_mx_down(const void* hc, const void* hs, const int32_t* off,
+                                        int64_t M, int32_t E, int64_t d, int64_t f, const void* wc,
+                                        const void* ws, const int32_t* rows, int64_t out_rows,
+                                        void* out, void* stream) {
+    if (cobalt_status st = check_experts(off, M, E, d, f, 32, rows, out_rows)) return st;
+    if (!rows_ok(wc) || !ws) return COBALT_EINVAL;
+    if (M > 0 && (!rows_ok(hc) || !hs || (out_rows > 0 && !rows_ok(out)))) return COBALT_EINVAL;
+    if (M == 0 || out_rows == 0) return COBALT_OK;
+    return launch_mx_down({off, E, (int32_t)M}, hc, hs, d, f, wc, ws, {rows, out_rows}, out,
+                          (hipStream_t)stream);
+}

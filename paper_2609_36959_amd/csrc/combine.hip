@@ -26,20 +26,6 @@
 namespace cobalt {
 namespace {
 
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-
-// Rounds a and b to bf16, nearest even, and packs them with a in the low
-// half: one v_cvt_pk_bf16_f32. In the floating-point mode of these kernels
-// (IEEE, fp32 denormals kept) it gives the bits of the IEEE-754 rule written
-// out (a quiet NaN keeps its sign and the top bits of its payload) on every
-// one of the 2^32 inputs, and costs one instruction where the bit rule
-// costs about ten for the pair.
-__device__ __forceinline__ uint32_t pack_bf16_rne(float a, float b) {
-    const f32x2 v = {a, b};
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
-}
-
 // How y_f32 is stored (store_sums chooses): in whole lines, non-temporally or
 // not, or by each thread at its own chunk. (They are kernels of their own: from
 // the two sides of a branch the compiler makes one ordinary store.)

@@ -1,0 +1,67 @@
+// Gradients of the combine:
+//   dexpert_out[pos[t][j]][c] = bf16_rne( gates[t][j] * dy[t][c] ),
+//   dgates[t][j] = sum_c dy[t][c] * expert_out[pos[t][j]][c] in fp32;
+// pairs whose row is outside [0, T*K) have no row and the gate gradient 0.
+#include <algorithm>
+
+#include "internal.hpp"
+
+namespace cobalt {
+namespace {
+
+// One workgroup per token, one wave per slot. A wave reads its row's chunks
+// before it writes them, so the gradient may take the rows' place.
+__global__ __launch_bounds__(kMaxK * 64) void combine_backward_kernel(
+    const u32x4* __restrict__ dy, const u32x4* eo, const int32_t* __restrict__ pos,
+    const float* __restrict__ gates, int64_t t0, int K, int64_t nch, int64_t TK, u32x4* deo,
+    float* __restrict__ dgates) {
+    const int64_t t = t0 + blockIdx.x;
+    const int j = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    const int p = pos[t * K + j];
+    const bool ok = p >= 0 && p < TK;
+    const float gate = deo ? gates[t * K + j] : 0.0f;
+    float sum = 0.0f;
+    if (ok) {
+        for (int64_t c = lane; c < nch; c += 64) {
+            const u32x4 g = dy[t * nch + c];
+            if (dgates) {
+                const u32x4 v = eo[(int64_t)p * nch + c];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    sum = __builtin_fmaf(__uint_as_float(g[q] << 16),
+                                         __uint_as_float(v[q] << 16), sum);
+                    sum = __builtin_fmaf(__uint_as_float(g[q] & 0xffff0000u),
+                                         __uint_as_float(v[q] & 0xffff0000u), sum);
+                }
+            }
+            if (deo) {
+                u32x4 o;
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    o[q] = pack_bf16_rne(gate * __uint_as_float(g[q] << 16),
+                                         gate * __uint_as_float(g[q] & 0xffff0000u));
+                deo[(int64_t)p * nch + c] = o;
+            }
+        }
+    }
+    if (!dgates) return;
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+    if (lane == 0) dgates[t * K + j] = sum;
+}
+
+}  // namespace
+
+cobalt_status launch_combine_backward(const void* dy, const void* eo, const int32_t* pos,
+                                      const float* gates, int64_t T, int K, int64_t d, void* deo,
+                                      float* dgates, hipStream_t s) {
+    for_token_ranges(T, K * 64, [&](int64_t t0, int64_t n) {
+        combine_backward_kernel<<<(unsigned)n, K * 64, 0, s>>>((const u32x4*)dy, (const u32x4*)eo,
+                                                               pos, gates, t0, K, d / 8, T * K,
+                                                               (u32x4*)deo, dgates);
+    });
+    COBALT_LAUNCH_CHECK();
+    return COBALT_OK;
+}
+
+}  // namespace cobalt

@@ -1,0 +1,129 @@
+// Internal declarations of the experts' products.
+#pragma once
+
+#include "internal.hpp"
+
+namespace cobalt {
+
+// Rows grouped by expert: places [off[e], off[e+1]) of M belong to expert e.
+struct Groups {
+    const int32_t* off;
+    int32_t E;
+    int32_t M;
+};
+
+// Rows of a buffer that the places name (idx NULL: place i is row i).
+struct Rows {
+    const int32_t* idx;
+    int64_t n;
+    // Row of a place, or -1 if it has none in the buffer.
+    __device__ __forceinline__ int64_t of(int64_t place) const {
+        const int64_t r = idx ? idx[place] : place;
+        return r >= 0 && r < n ? r : -1;
+    }
+};
+
+enum class Act { kSilu = COBALT_ACT_SILU, kGelu = COBALT_ACT_GELU };
+
+// a(g) and a'(g) in fp32. Both activations are g * sigmoid(z(g)): z = g for
+// SiLU, and z = 2 sqrt(2/pi) (g + 0.044715 g^3) for the tanh form of GELU,
+// since (1 + tanh(t)) / 2 = sigmoid(2t); so one exponential serves either.
+template <Act A>
+__device__ __forceinline__ float act_sigmoid(float g) {
+    const float z = A == Act::kSilu ? g : 1.5957691216057308f * (g + 0.044715f * g * g * g);
+    return 1.0f / (1.0f + __expf(-z));
+}
+template <Act A>
+__device__ __forceinline__ float act(float g) {
+    return g * act_sigmoid<A>(g);
+}
+template <Act A>
+__device__ __forceinline__ float act_slope(float g) {
+    const float s = act_sigmoid<A>(g);
+    const float slope = A == Act::kSilu ? 1.0f : 1.5957691216057308f * (1.0f + 0.134145f * g * g);
+    return s * (1.0f + g * slope * (1.0f - s));
+}
+
+// Tile `id` of the list of all experts' tiles of BM places: its expert and
+// places [lo, hi). False behind the last tile. Called by whole waves; every
+// wave gets the same answer. Each lane counts the tiles of a run of experts,
+// the wave scans the counts, and the lane that holds the tile is found by a
+// ballot, so that no list has to be made by a launch of its own. Offsets
+// outside [0, M] are taken as the nearest bound; whatever they are, the tile
+// lies in [0, M].
+struct Tile {
+    int32_t e, lo, hi;
+};
+__device__ __forceinline__ bool find_tile(const Groups& g, int BM, uint32_t id, Tile* out) {
+    const int lane = threadIdx.x & 63;
+    const int per = (g.E + 63) / 64;
+    const int e0 = min(lane * per, g.E), e1 = min(e0 + per, g.E);
+    const auto bound = [&](int e) { return min(max(g.off[e], 0), g.M); };
+    const auto tiles = [&](int lo, int hi) {
+        return hi > lo ? (uint32_t)(hi - lo + BM - 1) / (uint32_t)BM : 0u;
+    };
+    uint32_t own = 0;
+    int lo = bound(e0);
+    for (int e = e0; e < e1; ++e) {
+        const int hi = bound(e + 1);
+        own += tiles(lo, hi);
+        lo = hi;
+    }
+    uint32_t incl = own;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t up = __shfl_up(incl, o, 64);
+        if (lane >= o) incl += up;
+    }
+    const uint64_t hit = __ballot(id - (incl - own) < own);
+    if (hit == 0) return false;
+    const int src = __ffsll((unsigned long long)hit) - 1;
+    uint32_t left =
+        id - (uint32_t)__builtin_amdgcn_readlane((int)(incl - own), src);
+    int e = src * per;
+    lo = bound(e);
+    int hi = bound(e + 1);
+    while (left >= tiles(lo, hi)) {
+        left -= tiles(lo, hi);
+        ++e;
+        lo = hi;
+        hi = bound(e + 1);
+    }
+    out->e = e;
+    out->lo = lo + (int)left * BM;
+    out->hi = min(hi, out->lo + BM);
+    return true;
+}
+
+// Most tiles of BM places that M places of E experts can make.
+inline int64_t most_tiles(int64_t M, int E, int BM) {
+    return M / BM + std::min<int64_t>(E, M);
+}
+
+cobalt_status launch_gate_up(const Groups& g, const void* x, Rows rows, int64_t d, int64_t f,
+                             const void* w_in, Act act, void* h, void* gate_up, hipStream_t s);
+cobalt_status launch_down(const Groups& g, const void* h, int64_t d, int64_t f,
+                          const void* w_down, Rows rows, void* out, hipStream_t s);
+cobalt_status launch_down_gradient(const Groups& g, const void* dout, Rows rows, int64_t d,
+                                   int64_t f, const void* w_down, const void* gate_up, Act act,
+                                   void* dgate_up, hipStream_t s);
+cobalt_status launch_gate_up_gradient(const Groups& g, const void* dgate_up, int64_t d, int64_t f,
+                                      const void* w_in, Rows rows, void* dx, hipStream_t s);
+// dw[e] (+)= sum_i a[i] b[i]^T over the places of e: a [.][na], b [.][nb],
+// taken at place i, or at its row where the flag says so.
+cobalt_status launch_weight_gradient(const Groups& g, const void* a, int64_t na, bool a_rows,
+                                     const void* b, int64_t nb, bool b_rows, Rows rows, void* dw,
+                                     bool f32, bool add, void* ws, hipStream_t s);
+size_t expert_backward_workspace_bytes(int64_t M, int E, int64_t d, int64_t f);
+
+cobalt_status launch_mx_quantize(const void* x, int64_t R, int64_t n, void* codes, void* scales,
+                                 hipStream_t s);
+cobalt_status launch_mx_dequantize(const void* codes, const void* scales, int64_t R, int64_t n,
+                                   void* y, hipStream_t s);
+cobalt_status launch_mx_gate_up(const Groups& g, const void* xc, const void* xs, Rows rows,
+                                int64_t d, int64_t f, const void* wc, const void* ws, Act act,
+                                void* h, hipStream_t s);
+cobalt_status launch_mx_down(const Groups& g, const void* hc, const void* hs, int64_t d, int64_t f,
+                             const void* wc, const void* ws, Rows rows, void* out, hipStream_t s);
+
+}  // namespace cobalt

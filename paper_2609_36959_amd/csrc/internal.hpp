@@ -49,6 +49,20 @@ __device__ __forceinline__ void store_through(const u32x4& v, void* base, int32_
     __builtin_amdgcn_raw_buffer_store_b128(v, rs, offset, 0, kSc1);
 }
 
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+// Rounds a and b to bf16, nearest even, and packs them with a in the low
+// half: one v_cvt_pk_bf16_f32. In the floating-point mode of these kernels
+// (IEEE, fp32 denormals kept) it gives the bits of the IEEE-754 rule written
+// out (a quiet NaN keeps its sign and the top bits of its payload) on every
+// one of the 2^32 inputs, and costs one instruction where the bit rule
+// costs about ten for the pair.
+__device__ __forceinline__ uint32_t pack_bf16_rne(float a, float b) {
+    const f32x2 v = {a, b};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+}
+
 // x / y for 0 <= x < 2^17 and 1 <= y: (x + 1/2) / y lies at least 1 / (2y)
 // from an integer, and the product is off by less than x / y * 2^-22.
 struct SmallDiv {
@@ -246,6 +260,13 @@ cobalt_status launch_node_combine(const void* eo, const int32_t* pos, const int3
                                   const float* gates, const int32_t* node_pos, int64_t T, int K,
                                   int N, int gpn, int64_t d, void* partial, void* y,
                                   hipStream_t s);
+size_t expert_group_workspace_bytes(int64_t T, int K, int E);
+cobalt_status launch_expert_group(const int32_t* topk, const int32_t* pos, int64_t T, int K, int E,
+                                  int32_t* rows, int32_t* tokens, int32_t* offsets, void* ws,
+                                  hipStream_t s);
+cobalt_status launch_combine_backward(const void* dy, const void* eo, const int32_t* pos,
+                                      const float* gates, int64_t T, int K, int64_t d, void* deo,
+                                      float* dgates, hipStream_t s);
 size_t replica_load_workspace_bytes(int64_t T, int K, int E, int G);
 cobalt_status launch_replica_load(const int32_t* topk, const int32_t* assigned, int64_t T, int K,
                                   int E, int G, uint32_t* load, void* ws, size_t ws_bytes,
