@@ -1,179 +1,338 @@
-// The experts' products in bf16: plain form.
-#include "simple.hpp"
+// The experts' products in bf16 and their gradients.
+#include "tile.hpp"
 
 namespace cobalt {
 namespace {
 
-__device__ __forceinline__ float wide(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
-__device__ __forceinline__ uint16_t narrow(float v) { return (uint16_t)pack_bf16_rne(v, 0.0f); }
+__device__ __forceinline__ float low(uint32_t v) { return __uint_as_float(v << 16); }
+__device__ __forceinline__ float high(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
 
-// tmp[i][n] fp32-free form: one workgroup makes the gate tile, then the up tile
-template <Act A>
-__global__ __launch_bounds__(256) void gate_up_kernel(Groups g, const uint16_t* x, Rows rows,
-                                                      int64_t d, int64_t f, const uint16_t* w,
-                                                      uint16_t* h, uint16_t* gu) {
-    __shared__ float gate[kTile][kTile + 1];
-    const int nt = (int)((f + kTile - 1) / kTile);
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// Eight results as bf16.
+__device__ __forceinline__ u32x4 pack8(const f32x4& a, const f32x4& b) {
+    return u32x4{pack_bf16_rne(a[0], a[1]), pack_bf16_rne(a[2], a[3]), pack_bf16_rne(b[0], b[1]),
+                 pack_bf16_rne(b[2], b[3])};
+}
+__device__ __forceinline__ u32x2 pack4(const f32x4& a) {
+    return u32x2{pack_bf16_rne(a[0], a[1]), pack_bf16_rne(a[2], a[3])};
+}
+
+// Places [lo, hi) of a tile as rows of x for the operand q: a place without a
+// row reads `other`, any row of the same length, and its results are not used.
+template <int B>
+__device__ __forceinline__ void start_rows(RowOperand<B>& q, const Tile& t, const char* x,
+                                           const Rows& rows, const char* other, int64_t bytes) {
+    q.start(bytes, [&](int r) {
+        const int64_t at = rows.of(min(t.lo + r, t.hi - 1));
+        return at < 0 ? other : x + at * bytes;
+    });
+}
+
+// The weight rows of a tile of h: a wave's 64 rows are 32 gate rows and the
+// 32 up rows of the same columns, in the order that gives a lane eight
+// consecutive columns of both.
+template <int TM, Act A>
+__global__ __launch_bounds__(512) void gate_up_kernel(Groups g, uint32_t b0, const char* x,
+                                                      Rows rows, int64_t d, int64_t f,
+                                                      const char* w, uint16_t* h, uint16_t* gu) {
+    constexpr int kBM = TM * 16 * kWM;
+    __shared__ __attribute__((aligned(1024))) char lds[tile_lds(kBM)];
+    const TileAt at = tile_at(b0 + blockIdx.x, (uint32_t)((f + kBN / 2 - 1) / (kBN / 2)));
     Tile t;
-    if (!find_tile(g, kTile, blockIdx.x / nt, &t)) return;
-    const int64_t n0 = (int64_t)(blockIdx.x % nt) * kTile;
-    const auto a = [&](int m, int64_t k) {
-        const int64_t r = rows.of(t.lo + m);
-        return r < 0 ? (uint16_t)0 : x[r * d + k];
-    };
-    for (int side = 0; side < 2; ++side) {
-        const uint16_t* we = w + ((int64_t)t.e * 2 + side) * f * d;
-        simple_product(
-            t.hi - t.lo, n0, f, d, a, [&](int64_t n, int64_t k) { return we[n * d + k]; },
-            [&](int m, int64_t n, float v) {
-                const int64_t i = t.lo + m;
-                if (gu) gu[i * 2 * f + side * f + n] = narrow(v);
-                if (side == 0)
-                    gate[m][n - n0] = act<A>(v);
-                else
-                    h[i * f + n] = narrow(gate[m][n - n0] * v);
-            });
+    if (!find_tile(g, kBM, at.m, &t)) return;
+    const int64_t n0 = (int64_t)at.n * (kBN / 2);
+    const char* we = w + (int64_t)t.e * 2 * f * d * 2;
+    RowOperand<kBM> q;
+    RowOperand<kBN> p;
+    start_rows(q, t, x, rows, we, d * 2);
+    p.start(d * 2, [&](int r) {
+        const int i = r & 15, side = (r >> 5) & 1;
+        const int64_t n = n0 + (r >> 6) * 32 + (i >> 2) * 8 + ((r >> 4) & 1) * 4 + (i & 3);
+        return we + (side * f + (n < f ? n : f - 1)) * d * 2;
+    });
+    Acc<TM> acc;
+    multiply<TM>(lds, q, p, (int)((d * 2 + kStepBytes - 1) / kStepBytes), acc);
+    const int lane = threadIdx.x & 63, wv = wave_id();
+    const int64_t n = n0 + wv % kWN * 32 + (lane >> 4) * 8;
+    if (n >= f) return;
+#pragma unroll
+    for (int y = 0; y < TM; ++y) {
+        const int64_t i = t.lo + wv / kWN * (TM * 16) + y * 16 + (lane & 15);
+        if (i >= t.hi) continue;
+        if (rows.of(i) < 0)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) acc[y][k] = f32x4{0, 0, 0, 0};
+        if (gu) {
+            *(u32x4*)(gu + i * 2 * f + n) = pack8(acc[y][0], acc[y][1]);
+            *(u32x4*)(gu + i * 2 * f + f + n) = pack8(acc[y][2], acc[y][3]);
+        }
+        f32x4 v[2];
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            v[k / 4][k % 4] = act<A>(acc[y][k / 4][k % 4]) * acc[y][2 + k / 4][k % 4];
+        *(u32x4*)(h + i * f + n) = pack8(v[0], v[1]);
     }
 }
 
-__global__ __launch_bounds__(256) void down_kernel(Groups g, const uint16_t* h, int64_t d,
-                                                   int64_t f, const uint16_t* w, Rows rows,
+template <int TM>
+__global__ __launch_bounds__(512) void down_kernel(Groups g, uint32_t b0, const char* h, int64_t d,
+                                                   int64_t f, const char* w, Rows rows,
                                                    uint16_t* out) {
-    const int nt = (int)((d + kTile - 1) / kTile);
+    constexpr int kBM = TM * 16 * kWM;
+    __shared__ __attribute__((aligned(1024))) char lds[tile_lds(kBM)];
+    const TileAt at = tile_at(b0 + blockIdx.x, (uint32_t)((d + kBN - 1) / kBN));
     Tile t;
-    if (!find_tile(g, kTile, blockIdx.x / nt, &t)) return;
-    const uint16_t* we = w + (int64_t)t.e * d * f;
-    simple_product(
-        t.hi - t.lo, (int64_t)(blockIdx.x % nt) * kTile, d, f,
-        [&](int m, int64_t k) { return h[(int64_t)(t.lo + m) * f + k]; },
-        [&](int64_t n, int64_t k) { return we[n * f + k]; },
-        [&](int m, int64_t n, float v) {
-            const int64_t r = rows.of(t.lo + m);
-            if (r >= 0) out[r * d + n] = narrow(v);
-        });
+    if (!find_tile(g, kBM, at.m, &t)) return;
+    const int64_t n0 = (int64_t)at.n * kBN;
+    const char* we = w + (int64_t)t.e * d * f * 2;
+    RowOperand<kBM> q;
+    RowOperand<kBN> p;
+    start_rows(q, t, h, Rows{nullptr, g.M}, we, f * 2);
+    p.start(f * 2, [&](int r) {
+        const int i = r & 15;
+        const int64_t n = n0 + (r >> 6) * 64 + (i >> 2) * 16 + ((r >> 4) & 3) * 4 + (i & 3);
+        return we + (n < d ? n : d - 1) * f * 2;
+    });
+    Acc<TM> acc;
+    multiply<TM>(lds, q, p, (int)((f * 2 + kStepBytes - 1) / kStepBytes), acc);
+    const int lane = threadIdx.x & 63, wv = wave_id();
+    const int64_t n = n0 + wv % kWN * 64 + (lane >> 4) * 16;
+#pragma unroll
+    for (int y = 0; y < TM; ++y) {
+        const int64_t i = t.lo + wv / kWN * (TM * 16) + y * 16 + (lane & 15);
+        if (i >= t.hi) continue;
+        const int64_t r = rows.of(i);
+        if (r < 0) continue;
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            if (n + 8 * k < d)
+                *(u32x4*)(out + r * d + n + 8 * k) = pack8(acc[y][2 * k], acc[y][2 * k + 1]);
+    }
 }
 
-template <Act A>
-__global__ __launch_bounds__(256) void down_gradient_kernel(Groups g, const uint16_t* dout,
-                                                            Rows rows, int64_t d, int64_t f,
-                                                            const uint16_t* w,
+template <int TM, Act A>
+__global__ __launch_bounds__(512) void down_gradient_kernel(Groups g, uint32_t b0,
+                                                            const char* dout, Rows rows, int64_t d,
+                                                            int64_t f, const char* w,
                                                             const uint16_t* gu, uint16_t* dgu) {
-    const int nt = (int)((f + kTile - 1) / kTile);
+    constexpr int kBM = TM * 16 * kWM;
+    __shared__ __attribute__((aligned(1024))) char lds[tile_lds(kBM)];
+    const TileAt at = tile_at(b0 + blockIdx.x, (uint32_t)((f + kBN - 1) / kBN));
     Tile t;
-    if (!find_tile(g, kTile, blockIdx.x / nt, &t)) return;
-    const uint16_t* we = w + (int64_t)t.e * d * f;
-    simple_product(
-        t.hi - t.lo, (int64_t)(blockIdx.x % nt) * kTile, f, d,
-        [&](int m, int64_t k) {
-            const int64_t r = rows.of(t.lo + m);
-            return r < 0 ? (uint16_t)0 : dout[r * d + k];
-        },
-        [&](int64_t n, int64_t k) { return we[k * f + n]; },
-        [&](int m, int64_t n, float v) {
-            const int64_t i = t.lo + m;
-            const float gv = wide(gu[i * 2 * f + n]), uv = wide(gu[i * 2 * f + f + n]);
-            dgu[i * 2 * f + n] = narrow(v * uv * act_slope<A>(gv));
-            dgu[i * 2 * f + f + n] = narrow(v * act<A>(gv));
-        });
+    if (!find_tile(g, kBM, at.m, &t)) return;
+    const int64_t n0 = (int64_t)at.n * kBN;
+    const char* we = w + (int64_t)t.e * d * f * 2;
+    RowOperand<kBM> q;
+    ColumnOperand<kBN> p;
+    start_rows(q, t, dout, rows, we, d * 2);
+    p.start(we + n0 * 2, f - n0, f * 2, d, nullptr, d);
+    Acc<TM> acc;
+    multiply<TM>(lds, q, p, (int)((d * 2 + kStepBytes - 1) / kStepBytes), acc);
+    const int lane = threadIdx.x & 63, wv = wave_id();
+#pragma unroll
+    for (int y = 0; y < TM; ++y) {
+        const int64_t i = t.lo + wv / kWN * (TM * 16) + y * 16 + (lane & 15);
+        if (i >= t.hi) continue;
+        const bool ok = rows.of(i) >= 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int64_t n = n0 + wv % kWN * 64 + k * 16 + (lane >> 4) * 4;
+            if (n >= f) continue;
+            const u32x2 gb = *(const u32x2*)(gu + i * 2 * f + n);
+            const u32x2 ub = *(const u32x2*)(gu + i * 2 * f + f + n);
+            f32x4 dg, du;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const float gv = c & 1 ? high(gb[c / 2]) : low(gb[c / 2]);
+                const float uv = c & 1 ? high(ub[c / 2]) : low(ub[c / 2]);
+                const float v = ok ? acc[y][k][c] : 0.0f;
+                dg[c] = v * uv * act_slope<A>(gv);
+                du[c] = v * act<A>(gv);
+            }
+            *(u32x2*)(dgu + i * 2 * f + n) = pack4(dg);
+            *(u32x2*)(dgu + i * 2 * f + f + n) = pack4(du);
+        }
+    }
 }
 
-__global__ __launch_bounds__(256) void gate_up_gradient_kernel(Groups g, const uint16_t* dgu,
-                                                               int64_t d, int64_t f,
-                                                               const uint16_t* w, Rows rows,
+template <int TM>
+__global__ __launch_bounds__(512) void gate_up_gradient_kernel(Groups g, uint32_t b0,
+                                                               const char* dgu, int64_t d,
+                                                               int64_t f, const char* w, Rows rows,
                                                                uint16_t* dx) {
-    const int nt = (int)((d + kTile - 1) / kTile);
+    constexpr int kBM = TM * 16 * kWM;
+    __shared__ __attribute__((aligned(1024))) char lds[tile_lds(kBM)];
+    const TileAt at = tile_at(b0 + blockIdx.x, (uint32_t)((d + kBN - 1) / kBN));
     Tile t;
-    if (!find_tile(g, kTile, blockIdx.x / nt, &t)) return;
-    const uint16_t* we = w + (int64_t)t.e * 2 * f * d;
-    simple_product(
-        t.hi - t.lo, (int64_t)(blockIdx.x % nt) * kTile, d, 2 * f,
-        [&](int m, int64_t k) { return dgu[(int64_t)(t.lo + m) * 2 * f + k]; },
-        [&](int64_t n, int64_t k) { return we[k * d + n]; },
-        [&](int m, int64_t n, float v) {
-            const int64_t r = rows.of(t.lo + m);
-            if (r >= 0) dx[r * d + n] = narrow(v);
-        });
+    if (!find_tile(g, kBM, at.m, &t)) return;
+    const int64_t n0 = (int64_t)at.n * kBN;
+    const char* we = w + (int64_t)t.e * 2 * f * d * 2;
+    RowOperand<kBM> q;
+    ColumnOperand<kBN> p;
+    start_rows(q, t, dgu, Rows{nullptr, g.M}, we, f * 4);
+    p.start(we + n0 * 2, d - n0, d * 2, 2 * f, nullptr, 2 * f);
+    Acc<TM> acc;
+    multiply<TM>(lds, q, p, (int)((f * 4 + kStepBytes - 1) / kStepBytes), acc);
+    const int lane = threadIdx.x & 63, wv = wave_id();
+#pragma unroll
+    for (int y = 0; y < TM; ++y) {
+        const int64_t i = t.lo + wv / kWN * (TM * 16) + y * 16 + (lane & 15);
+        if (i >= t.hi) continue;
+        const int64_t r = rows.of(i);
+        if (r < 0) continue;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int64_t n = n0 + wv % kWN * 64 + k * 16 + (lane >> 4) * 4;
+            if (n < d) *(u32x2*)(dx + r * d + n) = pack4(acc[y][k]);
+        }
+    }
 }
 
-__global__ __launch_bounds__(256) void weight_gradient_kernel(Groups g, const uint16_t* a,
-                                                              int64_t na, bool a_rows,
-                                                              const uint16_t* b, int64_t nb,
-                                                              bool b_rows, Rows rows, void* dw,
-                                                              bool f32, bool add) {
-    const int nt = (int)((nb + kTile - 1) / kTile), mt = (int)((na + kTile - 1) / kTile);
-    const int e = blockIdx.x / (nt * mt), tile = blockIdx.x % (nt * mt);
-    const int64_t m0 = (int64_t)(tile / nt) * kTile;
+// Tiles of all experts' gradients, expert by expert.
+template <bool kFloat, bool kAdd>
+__global__ __launch_bounds__(512) void weight_gradient_kernel(Groups g, uint32_t b0, uint32_t mt,
+                                                              const char* a, int64_t na,
+                                                              Rows a_rows, const char* b,
+                                                              int64_t nb, Rows b_rows, void* dw) {
+    constexpr int TM = 8, kBM = TM * 16 * kWM;
+    __shared__ __attribute__((aligned(1024))) char lds[tile_lds(kBM)];
+    const TileAt at = tile_at(b0 + blockIdx.x, (uint32_t)((nb + kBN - 1) / kBN));
+    const uint32_t e = at.m / mt;
+    if (e >= (uint32_t)g.E) return;
+    const int64_t m0 = (int64_t)(at.m % mt) * kBM, n0 = (int64_t)at.n * kBN;
     const int lo = min(max(g.off[e], 0), g.M), hi = min(max(g.off[e + 1], 0), g.M);
-    simple_product(
-        (int)(na - m0 < kTile ? na - m0 : kTile), (int64_t)(tile % nt) * kTile, nb,
-        hi > lo ? hi - lo : 0,
-        [&](int m, int64_t k) {
-            const int64_t r = a_rows ? rows.of(lo + k) : lo + k;
-            return r < 0 ? (uint16_t)0 : a[r * na + m0 + m];
-        },
-        [&](int64_t n, int64_t k) {
-            const int64_t r = b_rows ? rows.of(lo + k) : lo + k;
-            return r < 0 ? (uint16_t)0 : b[r * nb + n];
-        },
-        [&](int m, int64_t n, float v) {
-            const int64_t at = ((int64_t)e * na + m0 + m) * nb + n;
-            if (!f32)
-                ((uint16_t*)dw)[at] = narrow(v);
-            else
-                ((float*)dw)[at] = add ? ((float*)dw)[at] + v : v;
-        });
+    Acc<TM> acc = {};
+    if (hi > lo) {
+        ColumnOperand<kBM> q;
+        ColumnOperand<kBN> p;
+        // without an index the places are the rows
+        const auto start = [&](auto& o, const char* v, int64_t n, int64_t c0, const Rows& rows) {
+            o.start(v + (rows.idx ? 0 : lo * n * 2) + c0 * 2, n - c0, n * 2, hi - lo,
+                    rows.idx ? rows.idx + lo : nullptr, rows.idx ? rows.n : hi - lo);
+        };
+        start(q, a, na, m0, a_rows);
+        start(p, b, nb, n0, b_rows);
+        multiply<TM>(lds, q, p, (hi - lo + 63) / 64, acc);
+    }
+    const int lane = threadIdx.x & 63, wv = wave_id();
+#pragma unroll
+    for (int y = 0; y < TM; ++y) {
+        const int64_t m = m0 + wv / kWN * (TM * 16) + y * 16 + (lane & 15);
+        if (m >= na) continue;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int64_t n = n0 + wv % kWN * 64 + k * 16 + (lane >> 4) * 4;
+            if (n >= nb) continue;
+            const int64_t i = ((int64_t)e * na + m) * nb + n;
+            if constexpr (!kFloat) {
+                *(u32x2*)((uint16_t*)dw + i) = pack4(acc[y][k]);
+            } else {
+                f32x4* to = (f32x4*)((float*)dw + i);
+                *to = kAdd ? *to + acc[y][k] : acc[y][k];
+            }
+        }
+    }
 }
 
-unsigned grid(const Groups& g, int64_t n) {
-    return (unsigned)(most_tiles(g.M, g.E, kTile) * ((n + kTile - 1) / kTile));
+// Launches `kernel(b0, workgroups)` over ranges of the workgroups of mt x nt
+// tiles that a grid can hold.
+template <typename F>
+cobalt_status over_tiles(int64_t mt, int64_t nt, F&& kernel) {
+    const int64_t all = tile_grid(mt, nt), most = kMaxLaunchItems / 512 / 256 * 256;
+    if (all > UINT32_MAX) return COBALT_EUNSUPPORTED;
+    for (int64_t b0 = 0; b0 < all; b0 += most) {
+        kernel((uint32_t)b0, (unsigned)std::min(all - b0, most));
+        COBALT_LAUNCH_CHECK();
+    }
+    return COBALT_OK;
 }
+
+// Calls f(TM) with the tiles' height for M places of E experts.
+template <typename F>
+cobalt_status by_height(const Groups& g, F&& f) {
+    const int64_t mean = g.M / g.E;
+    if (mean <= 64) return f(std::integral_constant<int, 2>());
+    if (mean <= 128) return f(std::integral_constant<int, 4>());
+    return f(std::integral_constant<int, 8>());
+}
+
+// Calls f(act) with the activation as a constant.
+template <typename F>
+auto by_act(Act a, F&& f) {
+    return a == Act::kSilu ? f(std::integral_constant<Act, Act::kSilu>())
+                           : f(std::integral_constant<Act, Act::kGelu>());
+}
+
+int64_t tiles(int64_t n, int64_t tile) { return (n + tile - 1) / tile; }
 
 }  // namespace
 
 cobalt_status launch_gate_up(const Groups& g, const void* x, Rows rows, int64_t d, int64_t f,
                              const void* w_in, Act act, void* h, void* gate_up, hipStream_t s) {
-    const auto k = act == Act::kSilu ? gate_up_kernel<Act::kSilu> : gate_up_kernel<Act::kGelu>;
-    k<<<grid(g, f), 256, 0, s>>>(g, (const uint16_t*)x, rows, d, f, (const uint16_t*)w_in,
-                                 (uint16_t*)h, (uint16_t*)gate_up);
-    COBALT_LAUNCH_CHECK();
-    return COBALT_OK;
+    return by_act(act, [&](auto a) {
+        return by_height(g, [&](auto tm) {
+            return over_tiles(most_tiles(g.M, g.E, tm * 32), tiles(f, kBN / 2),
+                              [&](uint32_t b0, unsigned n) {
+                                  gate_up_kernel<tm(), a()><<<n, 512, 0, s>>>(
+                                      g, b0, (const char*)x, rows, d, f, (const char*)w_in,
+                                      (uint16_t*)h, (uint16_t*)gate_up);
+                              });
+        });
+    });
 }
 
 cobalt_status launch_down(const Groups& g, const void* h, int64_t d, int64_t f,
                           const void* w_down, Rows rows, void* out, hipStream_t s) {
-    down_kernel<<<grid(g, d), 256, 0, s>>>(g, (const uint16_t*)h, d, f, (const uint16_t*)w_down,
-                                           rows, (uint16_t*)out);
-    COBALT_LAUNCH_CHECK();
-    return COBALT_OK;
+    return by_height(g, [&](auto tm) {
+        return over_tiles(most_tiles(g.M, g.E, tm * 32), tiles(d, kBN),
+                          [&](uint32_t b0, unsigned n) {
+                              down_kernel<tm()><<<n, 512, 0, s>>>(g, b0, (const char*)h, d, f,
+                                                                  (const char*)w_down, rows,
+                                                                  (uint16_t*)out);
+                          });
+    });
 }
 
 cobalt_status launch_down_gradient(const Groups& g, const void* dout, Rows rows, int64_t d,
                                    int64_t f, const void* w_down, const void* gate_up, Act act,
                                    void* dgate_up, hipStream_t s) {
-    const auto k =
-        act == Act::kSilu ? down_gradient_kernel<Act::kSilu> : down_gradient_kernel<Act::kGelu>;
-    k<<<grid(g, f), 256, 0, s>>>(g, (const uint16_t*)dout, rows, d, f, (const uint16_t*)w_down,
-                                 (const uint16_t*)gate_up, (uint16_t*)dgate_up);
-    COBALT_LAUNCH_CHECK();
-    return COBALT_OK;
+    return by_act(act, [&](auto a) {
+        return by_height(g, [&](auto tm) {
+            return over_tiles(most_tiles(g.M, g.E, tm * 32), tiles(f, kBN),
+                              [&](uint32_t b0, unsigned n) {
+                                  down_gradient_kernel<tm(), a()><<<n, 512, 0, s>>>(
+                                      g, b0, (const char*)dout, rows, d, f, (const char*)w_down,
+                                      (const uint16_t*)gate_up, (uint16_t*)dgate_up);
+                              });
+        });
+    });
 }
 
 cobalt_status launch_gate_up_gradient(const Groups& g, const void* dgate_up, int64_t d, int64_t f,
                                       const void* w_in, Rows rows, void* dx, hipStream_t s) {
-    gate_up_gradient_kernel<<<grid(g, d), 256, 0, s>>>(g, (const uint16_t*)dgate_up, d, f,
-                                                       (const uint16_t*)w_in, rows, (uint16_t*)dx);
-    COBALT_LAUNCH_CHECK();
-    return COBALT_OK;
+    return by_height(g, [&](auto tm) {
+        return over_tiles(most_tiles(g.M, g.E, tm * 32), tiles(d, kBN),
+                          [&](uint32_t b0, unsigned n) {
+                              gate_up_gradient_kernel<tm()><<<n, 512, 0, s>>>(
+                                  g, b0, (const char*)dgate_up, d, f, (const char*)w_in, rows,
+                                  (uint16_t*)dx);
+                          });
+    });
 }
 
 cobalt_status launch_weight_gradient(const Groups& g, const void* a, int64_t na, bool a_rows,
                                      const void* b, int64_t nb, bool b_rows, Rows rows, void* dw,
                                      bool f32, bool add, void* ws, hipStream_t s) {
-    const int64_t tiles = (na + kTile - 1) / kTile * ((nb + kTile - 1) / kTile);
-    weight_gradient_kernel<<<(unsigned)(tiles * g.E), 256, 0, s>>>(
-        g, (const uint16_t*)a, na, a_rows, (const uint16_t*)b, nb, b_rows, rows, dw, f32, add);
-    COBALT_LAUNCH_CHECK();
-    return COBALT_OK;
+    const Rows places{nullptr, g.M};
+    const int64_t mt = tiles(na, 256);
+    return over_tiles(mt * g.E, tiles(nb, kBN), [&](uint32_t b0, unsigned n) {
+        const auto k = !f32 ? weight_gradient_kernel<false, false>
+                       : add ? weight_gradient_kernel<true, true>
+                             : weight_gradient_kernel<true, false>;
+        k<<<n, 512, 0, s>>>(g, b0, (uint32_t)mt, (const char*)a, na, a_rows ? rows : places,
+                            (const char*)b, nb, b_rows ? rows : places, dw);
+    });
 }
 
 size_t expert_backward_workspace_bytes(int64_t, int, int64_t, int64_t) { return 256; }
