@@ -1,134 +1,28 @@
 // The experts' products in bf16 and their gradients.
-#include "tile.hpp"
+#include "forward.hpp"
 
 namespace cobalt {
 namespace {
 
-__device__ __forceinline__ float low(uint32_t v) { return __uint_as_float(v << 16); }
-__device__ __forceinline__ float high(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
-
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-
-// Eight results as bf16.
-__device__ __forceinline__ u32x4 pack8(const f32x4& a, const f32x4& b) {
-    return u32x4{pack_bf16_rne(a[0], a[1]), pack_bf16_rne(a[2], a[3]), pack_bf16_rne(b[0], b[1]),
-                 pack_bf16_rne(b[2], b[3])};
-}
-__device__ __forceinline__ u32x2 pack4(const f32x4& a) {
-    return u32x2{pack_bf16_rne(a[0], a[1]), pack_bf16_rne(a[2], a[3])};
-}
-
-// Places [lo, hi) of a tile as rows of x for the operand q: a place without a
-// row reads `other`, any row of the same length, and its results are not used.
-template <int B>
-__device__ __forceinline__ void start_rows(RowOperand<B>& q, const Tile& t, const char* x,
-                                           const Rows& rows, const char* other, int64_t bytes) {
-    q.start(bytes, [&](int r) {
-        const int64_t at = rows.of(min(t.lo + r, t.hi - 1));
-        return at < 0 ? other : x + at * bytes;
-    });
-}
-
-// The weight rows of a tile of h: a wave's 64 rows are 32 gate rows and the
-// 32 up rows of the same columns, in the order that gives a lane eight
-// consecutive columns of both.
-template <int TM, Act A>
-__global__ __launch_bounds__(512) void gate_up_kernel(Groups g, uint32_t b0, const char* x,
-                                                      Rows rows, int64_t d, int64_t f,
-                                                      const char* w, uint16_t* h, uint16_t* gu) {
-    constexpr int kBM = TM * 16 * kWM;
-    __shared__ __attribute__((aligned(1024))) char lds[tile_lds(kBM)];
-    const TileAt at = tile_at(b0 + blockIdx.x, (uint32_t)((f + kBN / 2 - 1) / (kBN / 2)));
-    Tile t;
-    if (!find_tile(g, kBM, at.m, &t)) return;
-    const int64_t n0 = (int64_t)at.n * (kBN / 2);
-    const char* we = w + (int64_t)t.e * 2 * f * d * 2;
-    RowOperand<kBM> q;
-    RowOperand<kBN> p;
-    start_rows(q, t, x, rows, we, d * 2);
-    p.start(d * 2, [&](int r) {
-        const int i = r & 15, side = (r >> 5) & 1;
-        const int64_t n = n0 + (r >> 6) * 32 + (i >> 2) * 8 + ((r >> 4) & 1) * 4 + (i & 3);
-        return we + (side * f + (n < f ? n : f - 1)) * d * 2;
-    });
-    Acc<TM> acc;
-    multiply<TM>(lds, q, p, (int)((d * 2 + kStepBytes - 1) / kStepBytes), acc);
-    const int lane = threadIdx.x & 63, wv = wave_id();
-    const int64_t n = n0 + wv % kWN * 32 + (lane >> 4) * 8;
-    if (n >= f) return;
-#pragma unroll
-    for (int y = 0; y < TM; ++y) {
-        const int64_t i = t.lo + wv / kWN * (TM * 16) + y * 16 + (lane & 15);
-        if (i >= t.hi) continue;
-        if (rows.of(i) < 0)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) acc[y][k] = f32x4{0, 0, 0, 0};
-        if (gu) {
-            *(u32x4*)(gu + i * 2 * f + n) = pack8(acc[y][0], acc[y][1]);
-            *(u32x4*)(gu + i * 2 * f + f + n) = pack8(acc[y][2], acc[y][3]);
-        }
-        f32x4 v[2];
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-            v[k / 4][k % 4] = act<A>(acc[y][k / 4][k % 4]) * acc[y][2 + k / 4][k % 4];
-        *(u32x4*)(h + i * f + n) = pack8(v[0], v[1]);
-    }
-}
-
-template <int TM>
-__global__ __launch_bounds__(512) void down_kernel(Groups g, uint32_t b0, const char* h, int64_t d,
-                                                   int64_t f, const char* w, Rows rows,
-                                                   uint16_t* out) {
-    constexpr int kBM = TM * 16 * kWM;
-    __shared__ __attribute__((aligned(1024))) char lds[tile_lds(kBM)];
-    const TileAt at = tile_at(b0 + blockIdx.x, (uint32_t)((d + kBN - 1) / kBN));
-    Tile t;
-    if (!find_tile(g, kBM, at.m, &t)) return;
-    const int64_t n0 = (int64_t)at.n * kBN;
-    const char* we = w + (int64_t)t.e * d * f * 2;
-    RowOperand<kBM> q;
-    RowOperand<kBN> p;
-    start_rows(q, t, h, Rows{nullptr, g.M}, we, f * 2);
-    p.start(f * 2, [&](int r) {
-        const int i = r & 15;
-        const int64_t n = n0 + (r >> 6) * 64 + (i >> 2) * 16 + ((r >> 4) & 3) * 4 + (i & 3);
-        return we + (n < d ? n : d - 1) * f * 2;
-    });
-    Acc<TM> acc;
-    multiply<TM>(lds, q, p, (int)((f * 2 + kStepBytes - 1) / kStepBytes), acc);
-    const int lane = threadIdx.x & 63, wv = wave_id();
-    const int64_t n = n0 + wv % kWN * 64 + (lane >> 4) * 16;
-#pragma unroll
-    for (int y = 0; y < TM; ++y) {
-        const int64_t i = t.lo + wv / kWN * (TM * 16) + y * 16 + (lane & 15);
-        if (i >= t.hi) continue;
-        const int64_t r = rows.of(i);
-        if (r < 0) continue;
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-            if (n + 8 * k < d)
-                *(u32x4*)(out + r * d + n + 8 * k) = pack8(acc[y][2 * k], acc[y][2 * k + 1]);
-    }
-}
-
-template <int TM, Act A>
+template <int TM, Act A, bool kWhole>
 __global__ __launch_bounds__(512) void down_gradient_kernel(Groups g, uint32_t b0,
                                                             const char* dout, Rows rows, int64_t d,
                                                             int64_t f, const char* w,
                                                             const uint16_t* gu, uint16_t* dgu) {
     constexpr int kBM = TM * 16 * kWM;
-    __shared__ __attribute__((aligned(1024))) char lds[tile_lds(kBM)];
+    __shared__ __attribute__((aligned(1024))) char lds[tile_lds<TM, Bf16Math<TM>>()];
     const TileAt at = tile_at(b0 + blockIdx.x, (uint32_t)((f + kBN - 1) / kBN));
     Tile t;
     if (!find_tile(g, kBM, at.m, &t)) return;
     const int64_t n0 = (int64_t)at.n * kBN;
     const char* we = w + (int64_t)t.e * d * f * 2;
-    RowOperand<kBM> q;
-    ColumnOperand<kBN> p;
+    RowOperand<kBM, false, kWhole> q;
+    ColumnOperand<kBN, kWhole> p;
     start_rows(q, t, dout, rows, we, d * 2);
     p.start(we + n0 * 2, f - n0, f * 2, d, nullptr, d);
     Acc<TM> acc;
-    multiply<TM>(lds, q, p, (int)((d * 2 + kStepBytes - 1) / kStepBytes), acc);
+    Bf16Math<TM> math;
+    multiply<TM>(lds, q, p, math, (int)((d * 2 + kStepBytes - 1) / kStepBytes), acc);
     const int lane = threadIdx.x & 63, wv = wave_id();
 #pragma unroll
     for (int y = 0; y < TM; ++y) {
@@ -156,24 +50,25 @@ __global__ __launch_bounds__(512) void down_gradient_kernel(Groups g, uint32_t b
     }
 }
 
-template <int TM>
+template <int TM, bool kWhole>
 __global__ __launch_bounds__(512) void gate_up_gradient_kernel(Groups g, uint32_t b0,
                                                                const char* dgu, int64_t d,
                                                                int64_t f, const char* w, Rows rows,
                                                                uint16_t* dx) {
     constexpr int kBM = TM * 16 * kWM;
-    __shared__ __attribute__((aligned(1024))) char lds[tile_lds(kBM)];
+    __shared__ __attribute__((aligned(1024))) char lds[tile_lds<TM, Bf16Math<TM>>()];
     const TileAt at = tile_at(b0 + blockIdx.x, (uint32_t)((d + kBN - 1) / kBN));
     Tile t;
     if (!find_tile(g, kBM, at.m, &t)) return;
     const int64_t n0 = (int64_t)at.n * kBN;
     const char* we = w + (int64_t)t.e * 2 * f * d * 2;
-    RowOperand<kBM> q;
-    ColumnOperand<kBN> p;
+    RowOperand<kBM, false, kWhole> q;
+    ColumnOperand<kBN, kWhole> p;
     start_rows(q, t, dgu, Rows{nullptr, g.M}, we, f * 4);
     p.start(we + n0 * 2, d - n0, d * 2, 2 * f, nullptr, 2 * f);
     Acc<TM> acc;
-    multiply<TM>(lds, q, p, (int)((f * 4 + kStepBytes - 1) / kStepBytes), acc);
+    Bf16Math<TM> math;
+    multiply<TM>(lds, q, p, math, (int)((f * 4 + kStepBytes - 1) / kStepBytes), acc);
     const int lane = threadIdx.x & 63, wv = wave_id();
 #pragma unroll
     for (int y = 0; y < TM; ++y) {
@@ -196,16 +91,17 @@ __global__ __launch_bounds__(512) void weight_gradient_kernel(Groups g, uint32_t
                                                               Rows a_rows, const char* b,
                                                               int64_t nb, Rows b_rows, void* dw) {
     constexpr int TM = 8, kBM = TM * 16 * kWM;
-    __shared__ __attribute__((aligned(1024))) char lds[tile_lds(kBM)];
+    __shared__ __attribute__((aligned(1024))) char lds[tile_lds<TM, Bf16Math<TM>>()];
     const TileAt at = tile_at(b0 + blockIdx.x, (uint32_t)((nb + kBN - 1) / kBN));
     const uint32_t e = at.m / mt;
     if (e >= (uint32_t)g.E) return;
     const int64_t m0 = (int64_t)(at.m % mt) * kBM, n0 = (int64_t)at.n * kBN;
     const int lo = min(max(g.off[e], 0), g.M), hi = min(max(g.off[e + 1], 0), g.M);
     Acc<TM> acc = {};
+    Bf16Math<TM> math;
     if (hi > lo) {
-        ColumnOperand<kBM> q;
-        ColumnOperand<kBN> p;
+        ColumnOperand<kBM, false> q;
+        ColumnOperand<kBN, false> p;
         // without an index the places are the rows
         const auto start = [&](auto& o, const char* v, int64_t n, int64_t c0, const Rows& rows) {
             o.start(v + (rows.idx ? 0 : lo * n * 2) + c0 * 2, n - c0, n * 2, hi - lo,
@@ -213,7 +109,7 @@ __global__ __launch_bounds__(512) void weight_gradient_kernel(Groups g, uint32_t
         };
         start(q, a, na, m0, a_rows);
         start(p, b, nb, n0, b_rows);
-        multiply<TM>(lds, q, p, (hi - lo + 63) / 64, acc);
+        multiply<TM>(lds, q, p, math, (hi - lo + 63) / 64, acc);
     }
     const int lane = threadIdx.x & 63, wv = wave_id();
 #pragma unroll
@@ -235,62 +131,23 @@ __global__ __launch_bounds__(512) void weight_gradient_kernel(Groups g, uint32_t
     }
 }
 
-// Launches `kernel(b0, workgroups)` over ranges of the workgroups of mt x nt
-// tiles that a grid can hold.
-template <typename F>
-cobalt_status over_tiles(int64_t mt, int64_t nt, F&& kernel) {
-    const int64_t all = tile_grid(mt, nt), most = kMaxLaunchItems / 512 / 256 * 256;
-    if (all > UINT32_MAX) return COBALT_EUNSUPPORTED;
-    for (int64_t b0 = 0; b0 < all; b0 += most) {
-        kernel((uint32_t)b0, (unsigned)std::min(all - b0, most));
-        COBALT_LAUNCH_CHECK();
-    }
-    return COBALT_OK;
-}
-
-// Calls f(TM) with the tiles' height for M places of E experts.
-template <typename F>
-cobalt_status by_height(const Groups& g, F&& f) {
-    const int64_t mean = g.M / g.E;
-    if (mean <= 64) return f(std::integral_constant<int, 2>());
-    if (mean <= 128) return f(std::integral_constant<int, 4>());
-    return f(std::integral_constant<int, 8>());
-}
-
-// Calls f(act) with the activation as a constant.
-template <typename F>
-auto by_act(Act a, F&& f) {
-    return a == Act::kSilu ? f(std::integral_constant<Act, Act::kSilu>())
-                           : f(std::integral_constant<Act, Act::kGelu>());
-}
-
-int64_t tiles(int64_t n, int64_t tile) { return (n + tile - 1) / tile; }
-
 }  // namespace
 
 cobalt_status launch_gate_up(const Groups& g, const void* x, Rows rows, int64_t d, int64_t f,
-                             const void* w_in, Act act, void* h, void* gate_up, hipStream_t s) {
-    return by_act(act, [&](auto a) {
-        return by_height(g, [&](auto tm) {
-            return over_tiles(most_tiles(g.M, g.E, tm * 32), tiles(f, kBN / 2),
-                              [&](uint32_t b0, unsigned n) {
-                                  gate_up_kernel<tm(), a()><<<n, 512, 0, s>>>(
-                                      g, b0, (const char*)x, rows, d, f, (const char*)w_in,
-                                      (uint16_t*)h, (uint16_t*)gate_up);
-                              });
-        });
+                             const void* w_in, Act act, void* h, void* gate_up_out,
+                             hipStream_t s) {
+    return by_bool(d % 64 == 0, [&](auto whole) {
+        typedef Bf16Rows<whole()> Side;
+        return gate_up(g, Side(x, nullptr, d), rows, Side(w_in, nullptr, d), f, act, h,
+                       gate_up_out, s);
     });
 }
 
 cobalt_status launch_down(const Groups& g, const void* h, int64_t d, int64_t f,
                           const void* w_down, Rows rows, void* out, hipStream_t s) {
-    return by_height(g, [&](auto tm) {
-        return over_tiles(most_tiles(g.M, g.E, tm * 32), tiles(d, kBN),
-                          [&](uint32_t b0, unsigned n) {
-                              down_kernel<tm()><<<n, 512, 0, s>>>(g, b0, (const char*)h, d, f,
-                                                                  (const char*)w_down, rows,
-                                                                  (uint16_t*)out);
-                          });
+    return by_bool(f % 64 == 0, [&](auto whole) {
+        typedef Bf16Rows<whole()> Side;
+        return down(g, Side(h, nullptr, f), Side(w_down, nullptr, f), d, rows, out, s);
     });
 }
 
@@ -298,26 +155,31 @@ cobalt_status launch_down_gradient(const Groups& g, const void* dout, Rows rows,
                                    int64_t f, const void* w_down, const void* gate_up, Act act,
                                    void* dgate_up, hipStream_t s) {
     return by_act(act, [&](auto a) {
-        return by_height(g, [&](auto tm) {
-            return over_tiles(most_tiles(g.M, g.E, tm * 32), tiles(f, kBN),
-                              [&](uint32_t b0, unsigned n) {
-                                  down_gradient_kernel<tm(), a()><<<n, 512, 0, s>>>(
-                                      g, b0, (const char*)dout, rows, d, f, (const char*)w_down,
-                                      (const uint16_t*)gate_up, (uint16_t*)dgate_up);
-                              });
+        return by_bool(d % 64 == 0, [&](auto whole) {
+            return by_height(g, [&](auto tm) {
+                return over_tiles(most_tiles(g.M, g.E, tm * 32), tiles(f, kBN),
+                                  [&](uint32_t b0, unsigned n) {
+                                      down_gradient_kernel<tm(), a(), whole()><<<n, 512, 0, s>>>(
+                                          g, b0, (const char*)dout, rows, d, f,
+                                          (const char*)w_down, (const uint16_t*)gate_up,
+                                          (uint16_t*)dgate_up);
+                                  });
+            });
         });
     });
 }
 
 cobalt_status launch_gate_up_gradient(const Groups& g, const void* dgate_up, int64_t d, int64_t f,
                                       const void* w_in, Rows rows, void* dx, hipStream_t s) {
-    return by_height(g, [&](auto tm) {
-        return over_tiles(most_tiles(g.M, g.E, tm * 32), tiles(d, kBN),
-                          [&](uint32_t b0, unsigned n) {
-                              gate_up_gradient_kernel<tm()><<<n, 512, 0, s>>>(
-                                  g, b0, (const char*)dgate_up, d, f, (const char*)w_in, rows,
-                                  (uint16_t*)dx);
-                          });
+    return by_bool(f % 32 == 0, [&](auto whole) {
+        return by_height(g, [&](auto tm) {
+            return over_tiles(most_tiles(g.M, g.E, tm * 32), tiles(d, kBN),
+                              [&](uint32_t b0, unsigned n) {
+                                  gate_up_gradient_kernel<tm(), whole()><<<n, 512, 0, s>>>(
+                                      g, b0, (const char*)dgate_up, d, f, (const char*)w_in, rows,
+                                      (uint16_t*)dx);
+                              });
+        });
     });
 }
 

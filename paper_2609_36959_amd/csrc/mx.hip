@@ -1,12 +1,10 @@
-// Microscaled 4-bit rows: quantisation, and the experts' products on them in
-// plain form.
-#include "simple.hpp"
+// Microscaled 4-bit rows: quantisation, and the experts' products on them.
+#include "forward.hpp"
 
 namespace cobalt {
 namespace {
 
 __device__ __forceinline__ float wide(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
-__device__ __forceinline__ uint16_t narrow(float v) { return (uint16_t)pack_bf16_rne(v, 0.0f); }
 
 // One thread per block of 32 values.
 __global__ __launch_bounds__(256) void quantize_kernel(const u32x4* __restrict__ x, int64_t blocks,
@@ -71,63 +69,6 @@ __global__ __launch_bounds__(256) void dequantize_kernel(const u32x4* __restrict
     }
 }
 
-// Value k of row r.
-struct MxRows {
-    const uint8_t* codes;
-    const uint8_t* scales;
-    int64_t n;
-    __device__ uint16_t operator()(int64_t r, int64_t k) const {
-        const uint32_t c = codes[(r * n + k) / 2] >> (k & 1 ? 4 : 0);
-        return narrow(e2m1(c & 15) * e8m0(scales[(r * n + k) / 32]));
-    }
-};
-
-template <Act A>
-__global__ __launch_bounds__(256) void gate_up_kernel(Groups g, MxRows x, Rows rows, int64_t d,
-                                                      int64_t f, MxRows w, uint16_t* h) {
-    __shared__ float gate[kTile][kTile + 1];
-    const int nt = (int)((f + kTile - 1) / kTile);
-    Tile t;
-    if (!find_tile(g, kTile, blockIdx.x / nt, &t)) return;
-    const int64_t n0 = (int64_t)(blockIdx.x % nt) * kTile;
-    for (int side = 0; side < 2; ++side) {
-        const int64_t w0 = ((int64_t)t.e * 2 + side) * f;
-        simple_product(
-            t.hi - t.lo, n0, f, d,
-            [&](int m, int64_t k) {
-                const int64_t r = rows.of(t.lo + m);
-                return r < 0 ? (uint16_t)0 : x(r, k);
-            },
-            [&](int64_t n, int64_t k) { return w(w0 + n, k); },
-            [&](int m, int64_t n, float v) {
-                if (side == 0)
-                    gate[m][n - n0] = act<A>(v);
-                else
-                    h[(int64_t)(t.lo + m) * f + n] = narrow(gate[m][n - n0] * v);
-            });
-    }
-}
-
-__global__ __launch_bounds__(256) void down_kernel(Groups g, MxRows h, int64_t d, int64_t f,
-                                                   MxRows w, Rows rows, uint16_t* out) {
-    const int nt = (int)((d + kTile - 1) / kTile);
-    Tile t;
-    if (!find_tile(g, kTile, blockIdx.x / nt, &t)) return;
-    const int64_t w0 = (int64_t)t.e * d;
-    simple_product(
-        t.hi - t.lo, (int64_t)(blockIdx.x % nt) * kTile, d, f,
-        [&](int m, int64_t k) { return h(t.lo + m, k); },
-        [&](int64_t n, int64_t k) { return w(w0 + n, k); },
-        [&](int m, int64_t n, float v) {
-            const int64_t r = rows.of(t.lo + m);
-            if (r >= 0) out[r * d + n] = narrow(v);
-        });
-}
-
-unsigned grid(const Groups& g, int64_t n) {
-    return (unsigned)(most_tiles(g.M, g.E, kTile) * ((n + kTile - 1) / kTile));
-}
-
 }  // namespace
 
 cobalt_status launch_mx_quantize(const void* x, int64_t R, int64_t n, void* codes, void* scales,
@@ -152,20 +93,18 @@ cobalt_status launch_mx_dequantize(const void* codes, const void* scales, int64_
 cobalt_status launch_mx_gate_up(const Groups& g, const void* xc, const void* xs, Rows rows,
                                 int64_t d, int64_t f, const void* wc, const void* ws, Act act,
                                 void* h, hipStream_t s) {
-    const auto k = act == Act::kSilu ? gate_up_kernel<Act::kSilu> : gate_up_kernel<Act::kGelu>;
-    k<<<grid(g, f), 256, 0, s>>>(g, MxRows{(const uint8_t*)xc, (const uint8_t*)xs, d}, rows, d, f,
-                                 MxRows{(const uint8_t*)wc, (const uint8_t*)ws, d}, (uint16_t*)h);
-    COBALT_LAUNCH_CHECK();
-    return COBALT_OK;
+    return by_bool(d % 256 == 0, [&](auto whole) {
+        typedef MxRows<whole()> Side;
+        return gate_up(g, Side(xc, xs, d), rows, Side(wc, ws, d), f, act, h, nullptr, s);
+    });
 }
 
 cobalt_status launch_mx_down(const Groups& g, const void* hc, const void* hs, int64_t d, int64_t f,
                              const void* wc, const void* ws, Rows rows, void* out, hipStream_t s) {
-    down_kernel<<<grid(g, d), 256, 0, s>>>(g, MxRows{(const uint8_t*)hc, (const uint8_t*)hs, f}, d,
-                                           f, MxRows{(const uint8_t*)wc, (const uint8_t*)ws, f},
-                                           rows, (uint16_t*)out);
-    COBALT_LAUNCH_CHECK();
-    return COBALT_OK;
+    return by_bool(f % 256 == 0, [&](auto whole) {
+        typedef MxRows<whole()> Side;
+        return down(g, Side(hc, hs, f), Side(wc, ws, f), d, rows, out, s);
+    });
 }
 
 }  // namespace cobalt

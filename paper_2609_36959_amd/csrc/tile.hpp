@@ -33,7 +33,7 @@ constexpr int kWaves = 8, kWM = 2, kWN = 4;  // waves of a workgroup, along m an
 constexpr int kBN = 256;
 constexpr int kStepBytes = 128;
 
-// What is loaded for k past the end of a row, on both sides of a product.
+// What is loaded for k past the end, on both sides of a product.
 alignas(16) static __device__ const uint32_t kNothing[4] = {0, 0, 0, 0};
 
 // 16 bytes per lane from `p` to the 1 KiB of LDS at `lds`, lane by lane.
@@ -50,42 +50,57 @@ __device__ __forceinline__ int wave_id() {
 // step of each a row of 128 bytes in LDS. The 16-byte chunk c of row r lies at
 // chunk c ^ (r / 2 % 8), so that the 16 rows that a quarter wave reads at one
 // chunk lie in 16 different groups of four banks.
-template <int B>
+// kWhole: the rows are whole steps, and no load has to look for their end.
+// kNear: the rows lie within 4 GiB from an address that is the same for a whole
+// wave, and a lane keeps 32-bit offsets; otherwise they are anywhere.
+template <int B, bool kNear, bool kWhole>
 struct RowOperand {
     static constexpr bool kColumns = false;
     static constexpr int kLoads = B / 8 / kWaves;
     static constexpr int kReads = 1;  // LDS reads per fragment
-    const char* p[kLoads];
+    typedef std::conditional_t<kNear, uint32_t, const char*> At;
+    At p[kLoads];
+    const char* base;
     int64_t bytes;
 
-    // row(r): address of row r of the tile
+    __device__ __forceinline__ static int row_of(int j) {
+        return (j * kWaves + wave_id()) * 8 + (threadIdx.x & 63) / 8;
+    }
+    // the lane's chunk of the step, the same in all of its rows
+    __device__ __forceinline__ static int chunk() {
+        return (threadIdx.x & 7) ^ ((row_of(0) >> 1) & 7);
+    }
+    // row(r): row r of the tile, as an offset from `first` or an address
     template <typename F>
-    __device__ void start(int64_t row_bytes, F&& row) {
-        const int lane = threadIdx.x & 63, w = wave_id();
+    __device__ __forceinline__ void start(int64_t row_bytes, const char* first, F&& row) {
         bytes = row_bytes;
+        base = first;
 #pragma unroll
-        for (int j = 0; j < kLoads; ++j) {
-            const int r = (j * kWaves + w) * 8 + lane / 8;
-            p[j] = (const char*)row(r) + ((lane & 7) ^ ((r >> 1) & 7)) * 16;
-        }
+        for (int j = 0; j < kLoads; ++j) p[j] = (At)row(row_of(j)) + chunk() * 16;
+    }
+    __device__ __forceinline__ const char* at(int j) const {
+        if constexpr (kNear)
+            return base + p[j];
+        else
+            return p[j];
     }
     __device__ __forceinline__ void load(char* lds, int s) {
-        const int lane = threadIdx.x & 63, w = wave_id();
-        const int64_t left = bytes - (int64_t)s * kStepBytes;
-        if (left >= kStepBytes) {
+        const int w = wave_id();
+        if (kWhole || chunk() * 16 < bytes - (int64_t)s * kStepBytes) {
 #pragma unroll
-            for (int j = 0; j < kLoads; ++j) load_to_lds(p[j], lds + (j * kWaves + w) * 1024);
+            for (int j = 0; j < kLoads; ++j) load_to_lds(at(j), lds + (j * kWaves + w) * 1024);
+        } else {  // behind the end of the rows: zeros, on both sides of a product
+#pragma unroll
+            for (int j = 0; j < kLoads; ++j)
+                *(u32x4*)(lds + (j * kWaves + w) * 1024 + (threadIdx.x & 63) * 16) =
+                    u32x4{0, 0, 0, 0};
+        }
+        if constexpr (kNear) {
+            base += kStepBytes;
         } else {
 #pragma unroll
-            for (int j = 0; j < kLoads; ++j) {
-                const int r = (j * kWaves + w) * 8 + lane / 8;
-                const int c = (lane & 7) ^ ((r >> 1) & 7);
-                load_to_lds(c * 16 < left ? p[j] : (const char*)kNothing,
-                            lds + (j * kWaves + w) * 1024);
-            }
+            for (int j = 0; j < kLoads; ++j) p[j] += kStepBytes;
         }
-#pragma unroll
-        for (int j = 0; j < kLoads; ++j) p[j] += kStepBytes;
     }
     // The wave's part of rows r0 + 16 t + (0..15) for half kk of the step: a
     // lane's chunk is 2 * (lane / 16) + kk.
@@ -101,7 +116,8 @@ struct RowOperand {
 // of their column by two transposing reads of four rows each. The 32-byte
 // unit u of row k lies at unit u ^ (k % 4 + k / 16 % 2 * 4): a half wave reads
 // one unit of eight rows, from eight different groups of eight banks.
-template <int B>
+// kWhole: k is a multiple of a step and the rows have no index.
+template <int B, bool kWhole>
 struct ColumnOperand {
     static constexpr bool kColumns = true;
     static constexpr int kRowBytes = 2 * B;
@@ -113,7 +129,7 @@ struct ColumnOperand {
     const int32_t* idx; // row of each k, or NULL
     int64_t n_rows;
     int32_t next[kLoads];  // idx of the rows of the step to come
-    int32_t at[kLoads];    // byte of the lane's chunk in the row
+    uint32_t at[kLoads];   // the lane's chunk: byte in the row, or in the step (kWhole)
 
     __device__ __forceinline__ static int row_of(int j) {
         return (j * kWaves + wave_id()) * (1024 / kRowBytes) + (threadIdx.x & 63) * 16 / kRowBytes;
@@ -127,13 +143,13 @@ struct ColumnOperand {
         rows = k;
         idx = index;
         n_rows = index_rows;
-        if (idx) fetch(0);
+        if (!kWhole && idx) fetch(0);
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
             const int r = row_of(j), slot = lane * 16 % kRowBytes / 16;
             const int unit = (slot >> 1) ^ ((r & 3) | (((r >> 4) & 1) << 2));
             const int c = (unit * 2 + (slot & 1)) * 8;
-            at[j] = (c < cols ? c : (int)cols - 8) * 2;
+            at[j] = (c < cols ? c : (int)cols - 8) * 2 + (kWhole ? r * (uint32_t)pitch : 0);
         }
     }
     __device__ __forceinline__ void fetch(int s) {
@@ -147,13 +163,20 @@ struct ColumnOperand {
         const int w = wave_id();
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
-            const int64_t k = (int64_t)s * 64 + row_of(j);
-            const int64_t r = idx ? next[j] : k;
-            const bool ok = k < rows && r >= 0 && r < n_rows;
-            load_to_lds(ok ? base + r * pitch + at[j] : (const char*)kNothing,
-                        lds + (j * kWaves + w) * 1024);
+            char* to = lds + (j * kWaves + w) * 1024;
+            if constexpr (kWhole) {
+                load_to_lds(base + at[j], to);
+            } else {
+                const int64_t k = (int64_t)s * 64 + row_of(j);
+                const int64_t r = idx ? next[j] : k;
+                const bool ok = k < rows && r >= 0 && r < n_rows;
+                load_to_lds(ok ? base + r * pitch + at[j] : (const char*)kNothing, to);
+            }
         }
-        if (idx) fetch(s + 1);
+        if constexpr (kWhole)
+            base += 64 * pitch;
+        else if (idx)
+            fetch(s + 1);
     }
     __device__ __forceinline__ static bf16x8 read(const char* lds, int c0, int t, int kk) {
         const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
@@ -171,34 +194,158 @@ struct ColumnOperand {
 template <int TM>
 using Acc = f32x4[TM][4];
 
-constexpr size_t tile_lds(int BM) { return 2 * (size_t)(BM + kBN) * kStepBytes; }
+// Products of bf16 fragments: 32 k at a time.
+template <int TM>
+struct Bf16Math {
+    static constexpr int kLds = 0, kReads = 0;
+    __device__ __forceinline__ void prefetch(int) {}
+    __device__ __forceinline__ void commit(char*, int) {}
+    __device__ __forceinline__ void read(const char*, int) {}
+    __device__ __forceinline__ void advance() {}
+    __device__ __forceinline__ f32x4 product(const bf16x8& p, const bf16x8& q, const f32x4& c,
+                                             int, int, int) const {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(p, q, c, 0, 0, 0);
+    }
+};
 
-template <int TM, typename Q, typename P>
-__device__ __forceinline__ void multiply(char* lds, Q& q, P& p, int steps, Acc<TM>& acc) {
+// Products of 4-bit fragments: 128 k at a time, with the scales of both
+// operands. A lane's chunk of 16 bytes is one block of 32 values, so it needs
+// one scale byte of its row for each half of a step, and the two are
+// neighbours. The eight scale bytes of a row and step come through registers
+// (rows of scales need not be aligned) into LDS, one dword per thread and
+// operand. There the two bytes of row r and chunk pair g lie next to those of
+// row r + 16 (r % 32 < 16), so that one dword serves a lane for two tiles.
+template <int TM, bool kWhole>
+struct MxMath {
+    static constexpr int kBM = TM * 16 * kWM;
+    static constexpr int kLds = 2 * (kBM + kBN) * 8, kReads = TM / 2 + 2;
+    const char* q;     // scales of the thread's row of q, at its dword of the step
+    const char* base;  // of the row of p: at a 32-bit offset from here
+    uint32_t p;
+    int left;          // bytes from there to the rows' end
+    uint32_t next_q, next_p;
+    uint32_t sq[2][TM / 2], sp[2][2];  // of this step, of the next
+
+    // row_q(r): scales of row r of q; row_p(r): of p, as an offset from `first`,
+    // the same for a wave; n: scales of a row
+    template <typename FQ, typename FP>
+    __device__ __forceinline__ void start(int64_t n, FQ&& row_q, const char* first, FP&& row_p) {
+        const int r = threadIdx.x / 2, at = threadIdx.x % 2 * 4;
+        q = (const char*)row_q(r < kBM ? r : kBM - 1) + at;
+        base = first;
+        p = (uint32_t)row_p(r) + at;
+        left = (int)n - at;
+    }
+    __device__ __forceinline__ static uint32_t dword(const char* p, int left) {
+        uint32_t v = 0;
+        if (kWhole || left >= 4) {
+            __builtin_memcpy(&v, p, 4);
+        } else {  // behind the row: 2^-127, for codes that are 0
+            if (left > 0) v = (uint8_t)p[0];
+            if (left > 1) v |= (uint32_t)(uint8_t)p[1] << 8;
+            if (left > 2) v |= (uint32_t)(uint8_t)p[2] << 16;
+        }
+        return v;
+    }
+    __device__ __forceinline__ void prefetch(int) {
+        if (kBM == 256 || threadIdx.x < kBM * 2) next_q = dword(q, left);
+        next_p = dword(base + p, left);
+        q += 8;
+        base += 8;
+        left -= 8;
+    }
+    __device__ __forceinline__ static void put(char* lds, uint32_t v) {
+        const int r = threadIdx.x / 2, g = threadIdx.x % 2 * 2;
+        uint16_t* to = (uint16_t*)lds + ((r / 32 * 16 + r % 16) * 4 + g) * 2 + r / 16 % 2;
+        to[0] = (uint16_t)v;
+        to[2] = (uint16_t)(v >> 16);
+    }
+    __device__ __forceinline__ void commit(char* lds, int s) {
+        char* to = lds + (s & 1) * (kLds / 2);
+        if (kBM == 256 || threadIdx.x < kBM * 2) put(to, next_q);
+        put(to + kBM * 8, next_p);
+    }
+    // the scales of step s, for both halves
+    __device__ __forceinline__ void read(const char* lds, int s) {
+        const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4, w = wave_id();
+        const char* at = lds + (s & 1) * (kLds / 2) + i * 16 + g * 4;
+        const char* aq = at + w / kWN * (TM * 16) * 8;
+        const char* ap = at + (kBM + w % kWN * 64) * 8;
+#pragma unroll
+        for (int t = 0; t < TM / 2; ++t) sq[1][t] = *(const uint32_t*)(aq + t * 256);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) sp[1][t] = *(const uint32_t*)(ap + t * 256);
+    }
+    __device__ __forceinline__ void advance() {
+#pragma unroll
+        for (int t = 0; t < TM / 2; ++t) sq[0][t] = sq[1][t];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) sp[0][t] = sp[1][t];
+    }
+    __device__ __forceinline__ f32x4 product(const bf16x8& pv, const bf16x8& qv, const f32x4& c,
+                                             int x, int t, int kk) const {
+        typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+        const i32x4 a4 = __builtin_bit_cast(i32x4, pv), b4 = __builtin_bit_cast(i32x4, qv);
+        // 4-bit operands take half of the registers
+        const auto a = __builtin_shufflevector(a4, a4, 0, 1, 2, 3, -1, -1, -1, -1);
+        const auto b = __builtin_shufflevector(b4, b4, 0, 1, 2, 3, -1, -1, -1, -1);
+        // byte of the scales: half kk of an even or odd tile
+        const auto mul = [&](auto bp, auto bq) {
+            constexpr int kFp4 = 4;
+            return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+                a, b, c, kFp4, kFp4, bp(), (int)sp[0][t / 2], bq(), (int)sq[0][x / 2]);
+        };
+        const auto by_q = [&](auto bp) {
+            const int n = kk + 2 * (x & 1);
+            return n == 0   ? mul(bp, std::integral_constant<int, 0>())
+                   : n == 1 ? mul(bp, std::integral_constant<int, 1>())
+                   : n == 2 ? mul(bp, std::integral_constant<int, 2>())
+                            : mul(bp, std::integral_constant<int, 3>());
+        };
+        const int n = kk + 2 * (t & 1);
+        return n == 0   ? by_q(std::integral_constant<int, 0>())
+               : n == 1 ? by_q(std::integral_constant<int, 1>())
+               : n == 2 ? by_q(std::integral_constant<int, 2>())
+                        : by_q(std::integral_constant<int, 3>());
+    }
+};
+
+// LDS of a tile: two stages, and what the products need besides.
+template <int TM, typename Math>
+constexpr size_t tile_lds() {
+    return 2 * (size_t)(TM * 16 * kWM + kBN) * kStepBytes + Math::kLds;
+}
+
+template <int TM, typename Q, typename P, typename Math>
+__device__ __forceinline__ void multiply(char* lds, Q& q, P& p, Math& math, int steps,
+                                         Acc<TM>& acc) {
     constexpr int kBM = TM * 16 * kWM, kStage = (kBM + kBN) * kStepBytes;
     const int w = wave_id(), m0 = w / kWN * (TM * 16), n0 = w % kWN * 64;
+    char* extra = lds + 2 * kStage;
     bf16x8 fq[2][TM], fp[2][4];
     const auto load = [&](int s) {
         char* at = lds + (s & 1) * kStage;
+        math.prefetch(s);
         q.load(at, s);
         p.load(at + kBM * kStepBytes, s);
     };
     const auto read = [&](int to, int s, int kk) {
         const char* at = lds + (s & 1) * kStage;
+        if (kk == 0) math.read(extra, s);
 #pragma unroll
         for (int t = 0; t < 4; ++t) fp[to][t] = P::read(at + kBM * kStepBytes, n0, t, kk);
 #pragma unroll
         for (int t = 0; t < TM; ++t) fq[to][t] = Q::read(at, m0, t, kk);
     };
-    const auto half = [&](int of, int s, int kk) {
-        read(of ^ 1, s, kk);
+    // the products of half kk, and the reads of the half after it
+    const auto half = [&](int kk, int s) {
+        read(kk ^ 1, s + kk, kk ^ 1);
 #pragma unroll
         for (int x = 0; x < TM; ++x)
 #pragma unroll
             for (int t = 0; t < 4; ++t)
-                acc[x][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp[of][t], fq[of][x],
-                                                                    acc[x][t], 0, 0, 0);
-        constexpr int kR = TM * Q::kReads + 4 * P::kReads, kM = 4 * TM;
+                acc[x][t] = math.product(fp[kk][t], fq[kk][x], acc[x][t], x, t, kk);
+        constexpr int kR = TM * Q::kReads + 4 * P::kReads + Math::kReads, kM = 4 * TM;
         constexpr int kPer = kM / kR > 0 ? kM / kR : 1;
         constexpr int kGroups = kM / kPer < kR ? kM / kPer : kR;
 #pragma unroll
@@ -206,6 +353,12 @@ __device__ __forceinline__ void multiply(char* lds, Q& q, P& p, int steps, Acc<T
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);    // a read of LDS
             __builtin_amdgcn_sched_group_barrier(0x008, kPer, 0);  // kPer products
         }
+        // holds the products here: nothing else would keep the compiler from
+        // moving them past the barrier, behind the wait that they should fill
+#pragma unroll
+        for (int x = 0; x < TM; ++x)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) asm volatile("" : "+v"(acc[x][t]));
         __builtin_amdgcn_sched_barrier(0);
     };
 #pragma unroll
@@ -213,16 +366,21 @@ __device__ __forceinline__ void multiply(char* lds, Q& q, P& p, int steps, Acc<T
 #pragma unroll
         for (int t = 0; t < 4; ++t) acc[x][t] = f32x4{0, 0, 0, 0};
     load(0);
+    math.commit(extra, 0);
     if (steps > 1) load(1);
-    asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     read(0, 0, 0);
+    math.advance();
     for (int s = 0; s < steps; ++s) {
-        half(0, s, 1);
+        half(0, s);
         // every wave has read stage s and has its part of stage s + 1
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        math.commit(extra, s + 1);
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         if (s + 2 < steps) load(s + 2);
         __builtin_amdgcn_sched_barrier(0);
-        half(1, s + 1, 0);  // behind the last step: reads that nothing uses
+        half(1, s);  // behind the last step: reads that nothing uses
+        math.advance();
     }
     // no wave still reads LDS when the tile's results go through it
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -244,5 +402,67 @@ __device__ __forceinline__ TileAt tile_at(uint32_t b, uint32_t nt) {
 inline int64_t tile_grid(int64_t mt, int64_t nt) {
     return ((mt + 3) / 4 * 4 * nt + 255) / 256 * 256;
 }
+
+__device__ __forceinline__ float low(uint32_t v) { return __uint_as_float(v << 16); }
+__device__ __forceinline__ float high(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// Eight results as bf16.
+__device__ __forceinline__ u32x4 pack8(const f32x4& a, const f32x4& b) {
+    return u32x4{pack_bf16_rne(a[0], a[1]), pack_bf16_rne(a[2], a[3]), pack_bf16_rne(b[0], b[1]),
+                 pack_bf16_rne(b[2], b[3])};
+}
+__device__ __forceinline__ u32x2 pack4(const f32x4& a) {
+    return u32x2{pack_bf16_rne(a[0], a[1]), pack_bf16_rne(a[2], a[3])};
+}
+
+// Places [lo, hi) of a tile as rows of x for the operand q: a place without a
+// row reads `other`, any row of the same length, and its results are not used.
+template <int B, bool kWhole>
+__device__ __forceinline__ void start_rows(RowOperand<B, false, kWhole>& q, const Tile& t, const char* x,
+                                           const Rows& rows, const char* other, int64_t bytes) {
+    q.start(bytes, nullptr, [&](int r) {
+        const int64_t at = rows.of(min(t.lo + r, t.hi - 1));
+        return at < 0 ? other : x + at * bytes;
+    });
+}
+
+// Launches `kernel(b0, workgroups)` over ranges of the workgroups of mt x nt
+// tiles that a grid can hold.
+template <typename F>
+cobalt_status over_tiles(int64_t mt, int64_t nt, F&& kernel) {
+    const int64_t all = tile_grid(mt, nt), most = kMaxLaunchItems / 512 / 256 * 256;
+    if (all > UINT32_MAX) return COBALT_EUNSUPPORTED;
+    for (int64_t b0 = 0; b0 < all; b0 += most) {
+        kernel((uint32_t)b0, (unsigned)std::min(all - b0, most));
+        COBALT_LAUNCH_CHECK();
+    }
+    return COBALT_OK;
+}
+
+// Calls f(TM) with the tiles' height for M places of E experts.
+template <typename F>
+cobalt_status by_height(const Groups& g, F&& f) {
+    const int64_t mean = g.M / g.E;
+    if (mean <= 64) return f(std::integral_constant<int, 2>());
+    if (mean <= 128) return f(std::integral_constant<int, 4>());
+    return f(std::integral_constant<int, 8>());
+}
+
+// Calls f(act) with the activation as a constant.
+template <typename F>
+auto by_act(Act a, F&& f) {
+    return a == Act::kSilu ? f(std::integral_constant<Act, Act::kSilu>())
+                           : f(std::integral_constant<Act, Act::kGelu>());
+}
+
+// Calls f(b) with b as a constant.
+template <typename F>
+auto by_bool(bool b, F&& f) {
+    return b ? f(std::integral_constant<bool, true>()) : f(std::integral_constant<bool, false>());
+}
+
+inline int64_t tiles(int64_t n, int64_t tile) { return (n + tile - 1) / tile; }
 
 }  // namespace cobalt
