@@ -1,5 +1,5 @@
 // The experts' products in bf16 and their gradients.
-#include "forward.hpp"
+#include "few.hpp"
 
 namespace cobalt {
 namespace {

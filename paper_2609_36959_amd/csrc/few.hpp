@@ -1,0 +1,229 @@
+// The experts' forward products for few rows per expert (single tokens of a
+// serving program): the weights are read once and little else happens, so a
+// workgroup takes 16 places and streams the weights from memory to registers.
+//
+// A wave multiplies 16 weight rows (gate_up: 16 gate and 16 up rows) with the
+// places' rows over a part of k: 64 bytes of each row a step, one 16-byte
+// chunk per lane, loads of kAhead steps in flight before their products. The
+// eight waves are KS parts of k by 8 / KS groups of 16 rows, KS the largest
+// that leaves a wave kLeast steps; their sums meet in LDS and are added in
+// the order of the parts.
+#pragma once
+
+#include "forward.hpp"
+
+namespace cobalt {
+
+constexpr int kFewPlaces = 16;  // places of a tile
+constexpr int kAhead = 4, kLeast = 8;
+
+// A lane's chunk of a fragment, with its scale where there are scales.
+struct Bf16Chunk {
+    u32x4 v;
+    template <typename Side>
+    __device__ __forceinline__ void load(const Side& s, int64_t row, int c) {
+        v = *(const u32x4*)(s.row(row) + c * 16);
+    }
+    __device__ __forceinline__ void clear() { v = u32x4{0, 0, 0, 0}; }
+    __device__ __forceinline__ static f32x4 product(const Bf16Chunk& p, const Bf16Chunk& q,
+                                                    const f32x4& c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, p.v),
+                                                       __builtin_bit_cast(bf16x8, q.v), c, 0, 0,
+                                                       0);
+    }
+};
+struct MxChunk {
+    u32x4 v;
+    int scale;
+    template <typename Side>
+    __device__ __forceinline__ void load(const Side& s, int64_t row, int c) {
+        v = *(const u32x4*)(s.row(row) + c * 16);
+        scale = (uint8_t)s.scale_row(row)[c];
+    }
+    __device__ __forceinline__ void clear() {
+        v = u32x4{0, 0, 0, 0};
+        scale = 0;
+    }
+    __device__ __forceinline__ static f32x4 product(const MxChunk& p, const MxChunk& q,
+                                                    const f32x4& c) {
+        return mx_product<0, 0>(__builtin_bit_cast(bf16x8, p.v), __builtin_bit_cast(bf16x8, q.v),
+                                c, p.scale, q.scale);
+    }
+};
+
+// sums[part][group][s][m][n] of the workgroup's waves: S weight rows per lane,
+// row[s] of w, times place row `at` of x (-1: weights in its place).
+template <int KS, int S, typename Side>
+__device__ __forceinline__ void stream_products(float* sums, const Side& x, int64_t at,
+                                                const Side& w, const int64_t (&row)[S]) {
+    typedef std::conditional_t<Side::kScaled, MxChunk, Bf16Chunk> Chunk;
+    const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4, wv = wave_id();
+    const int chunks = (int)(w.bytes / 16), steps = (chunks + 3) / 4;
+    const int per = (steps + KS - 1) / KS, part = wv % KS;
+    const int s0 = part * per, s1 = min(s0 + per, steps);
+    const bool none = at < 0;
+    const Side& from = none ? w : x;
+    const int64_t q_row = none ? row[0] : at;
+    Chunk p[2][kAhead][S], q[2][kAhead];
+    f32x4 acc[S];
+#pragma unroll
+    for (int k = 0; k < S; ++k) acc[k] = f32x4{0, 0, 0, 0};
+    // behind the last chunk: the last one again, and no product of it
+    const auto load = [&](int to, int s) {
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a) {
+            const int c = min((s + a) * 4 + g, chunks - 1);
+#pragma unroll
+            for (int k = 0; k < S; ++k) p[to][a][k].load(w, row[k], c);
+            q[to][a].load(from, q_row, c);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    const auto multiply = [&](int of, int s) {
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a) {
+            if (s + a >= s1) break;
+            if (!Side::kWhole && (s + a) * 4 + g >= chunks) {
+                q[of][a].clear();
+#pragma unroll
+                for (int k = 0; k < S; ++k) p[of][a][k].clear();
+            }
+#pragma unroll
+            for (int k = 0; k < S; ++k) acc[k] = Chunk::product(p[of][a][k], q[of][a], acc[k]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    if (s0 < s1) {
+        load(0, s0);
+        for (int s = s0; s < s1; s += 2 * kAhead) {
+            load(1, s + kAhead);
+            multiply(0, s);
+            if (s + kAhead >= s1) break;
+            load(0, s + 2 * kAhead);
+            multiply(1, s + kAhead);
+        }
+    }
+    float* to = sums + ((part * (kWaves / KS) + wv / KS) * S) * 256 + i * 16 + g * 4;
+#pragma unroll
+    for (int k = 0; k < S; ++k) *(f32x4*)(to + k * 256) = acc[k];
+    __syncthreads();
+}
+
+// The sum over the parts of value (m, n) of group `group`.
+template <int KS, int S>
+__device__ __forceinline__ float joined(const float* sums, int group, int k, int m, int n) {
+    float v = 0.0f;
+#pragma unroll
+    for (int part = 0; part < KS; ++part)
+        v += sums[((part * (kWaves / KS) + group) * S + k) * 256 + m * 16 + n];
+    return v;
+}
+
+template <int KS, Act A, typename Side>
+__global__ __launch_bounds__(512) void gate_up_few_kernel(Groups g, uint32_t b0, Side x, Rows rows,
+                                                          Side w, int64_t f, uint16_t* h,
+                                                          uint16_t* gu) {
+    constexpr int kCols = 16 * (kWaves / KS);
+    __shared__ __attribute__((aligned(16))) float sums[kWaves * 2 * 256];
+    const uint32_t nt = (uint32_t)((f + kCols - 1) / kCols), b = b0 + blockIdx.x;
+    Tile t;
+    if (!find_tile(g, kFewPlaces, b / nt, &t)) return;
+    const int64_t n0 = (int64_t)(b % nt) * kCols;
+    const int i = threadIdx.x & 15, group = wave_id() / KS;
+    const int64_t n = min(n0 + group * 16 + i, f - 1), first = (int64_t)t.e * 2 * f + n;
+    stream_products<KS, 2>(sums, x, rows.of(min(t.lo + i, t.hi - 1)), w, {first, first + f});
+    for (int k = threadIdx.x; k < kCols * (t.hi - t.lo); k += 512) {
+        const int m = k / kCols, c = k % kCols;
+        if (n0 + c >= f) continue;
+        const int64_t at = t.lo + m;
+        const bool ok = rows.of(at) >= 0;
+        const float gv = ok ? joined<KS, 2>(sums, c / 16, 0, m, c % 16) : 0.0f;
+        const float uv = ok ? joined<KS, 2>(sums, c / 16, 1, m, c % 16) : 0.0f;
+        if (gu) {
+            gu[at * 2 * f + n0 + c] = (uint16_t)pack_bf16_rne(gv, 0.0f);
+            gu[at * 2 * f + f + n0 + c] = (uint16_t)pack_bf16_rne(uv, 0.0f);
+        }
+        h[at * f + n0 + c] = (uint16_t)pack_bf16_rne(act<A>(gv) * uv, 0.0f);
+    }
+}
+
+template <int KS, typename Side>
+__global__ __launch_bounds__(512) void down_few_kernel(Groups g, uint32_t b0, Side h, Side w,
+                                                       int64_t d, Rows rows, uint16_t* out) {
+    constexpr int kCols = 16 * (kWaves / KS);
+    __shared__ __attribute__((aligned(16))) float sums[kWaves * 256];
+    const uint32_t nt = (uint32_t)((d + kCols - 1) / kCols), b = b0 + blockIdx.x;
+    Tile t;
+    if (!find_tile(g, kFewPlaces, b / nt, &t)) return;
+    const int64_t n0 = (int64_t)(b % nt) * kCols;
+    const int i = threadIdx.x & 15, group = wave_id() / KS;
+    const int64_t n = min(n0 + group * 16 + i, d - 1);
+    stream_products<KS, 1>(sums, h, min(t.lo + i, t.hi - 1), w, {t.e * d + n});
+    for (int k = threadIdx.x; k < kCols * (t.hi - t.lo); k += 512) {
+        const int m = k / kCols, c = k % kCols;
+        const int64_t r = rows.of(t.lo + m);
+        if (n0 + c >= d || r < 0) continue;
+        out[r * d + n0 + c] =
+            (uint16_t)pack_bf16_rne(joined<KS, 1>(sums, c / 16, 0, m, c % 16), 0.0f);
+    }
+}
+
+// Calls f(KS) for rows of `bytes` bytes.
+template <typename F>
+cobalt_status by_parts(int64_t bytes, F&& f) {
+    const int64_t steps = (bytes + 63) / 64;
+    if (steps >= 8 * kLeast) return f(std::integral_constant<int, 8>());
+    if (steps >= 4 * kLeast) return f(std::integral_constant<int, 4>());
+    if (steps >= 2 * kLeast) return f(std::integral_constant<int, 2>());
+    return f(std::integral_constant<int, 1>());
+}
+
+// Whether the products of M places of E experts stream the weights.
+inline bool few_rows(const Groups& g) { return g.M <= 16 * (int64_t)g.E; }
+
+// Workgroups for n columns.
+inline int64_t few_grid(const Groups& g, int64_t n, int ks) {
+    return most_tiles(g.M, g.E, kFewPlaces) * tiles(n, 16 * (kWaves / ks));
+}
+
+template <typename Side>
+cobalt_status gate_up(const Groups& g, const Side& x, Rows rows, const Side& w, int64_t f, Act act,
+                      void* h, void* gu, hipStream_t s) {
+    return by_act(act, [&](auto a) {
+        if (few_rows(g))
+            return by_parts(w.bytes, [&](auto ks) {
+                return over_tiles(few_grid(g, f, ks()), [&](uint32_t b0, unsigned n) {
+                    gate_up_few_kernel<ks(), a(), Side><<<n, 512, 0, s>>>(
+                        g, b0, x, rows, w, f, (uint16_t*)h, (uint16_t*)gu);
+                });
+            });
+        return by_height(g, [&](auto tm) {
+            return over_tiles(most_tiles(g.M, g.E, tm * 32), tiles(f, kBN / 2),
+                              [&](uint32_t b0, unsigned n) {
+                                  gate_up_kernel<tm(), a(), Side><<<n, 512, 0, s>>>(
+                                      g, b0, x, rows, w, f, (uint16_t*)h, (uint16_t*)gu);
+                              });
+        });
+    });
+}
+
+template <typename Side>
+cobalt_status down(const Groups& g, const Side& h, const Side& w, int64_t d, Rows rows, void* out,
+                   hipStream_t s) {
+    if (few_rows(g))
+        return by_parts(w.bytes, [&](auto ks) {
+            return over_tiles(few_grid(g, d, ks()), [&](uint32_t b0, unsigned n) {
+                down_few_kernel<ks(), Side>
+                    <<<n, 512, 0, s>>>(g, b0, h, w, d, rows, (uint16_t*)out);
+            });
+        });
+    return by_height(g, [&](auto tm) {
+        return over_tiles(most_tiles(g.M, g.E, tm * 32), tiles(d, kBN),
+                          [&](uint32_t b0, unsigned n) {
+                              down_kernel<tm(), Side>
+                                  <<<n, 512, 0, s>>>(g, b0, h, w, d, rows, (uint16_t*)out);
+                          });
+    });
+}
+
+}  // namespace cobalt

@@ -148,30 +148,4 @@ __global__ __launch_bounds__(512) void down_kernel(Groups g, uint32_t b0, Side h
     }
 }
 
-template <typename Side>
-cobalt_status gate_up(const Groups& g, const Side& x, Rows rows, const Side& w, int64_t f, Act act,
-                      void* h, void* gu, hipStream_t s) {
-    return by_act(act, [&](auto a) {
-        return by_height(g, [&](auto tm) {
-            return over_tiles(most_tiles(g.M, g.E, tm * 32), tiles(f, kBN / 2),
-                              [&](uint32_t b0, unsigned n) {
-                                  gate_up_kernel<tm(), a(), Side><<<n, 512, 0, s>>>(
-                                      g, b0, x, rows, w, f, (uint16_t*)h, (uint16_t*)gu);
-                              });
-        });
-    });
-}
-
-template <typename Side>
-cobalt_status down(const Groups& g, const Side& h, const Side& w, int64_t d, Rows rows, void* out,
-                   hipStream_t s) {
-    return by_height(g, [&](auto tm) {
-        return over_tiles(most_tiles(g.M, g.E, tm * 32), tiles(d, kBN),
-                          [&](uint32_t b0, unsigned n) {
-                              down_kernel<tm(), Side>
-                                  <<<n, 512, 0, s>>>(g, b0, h, w, d, rows, (uint16_t*)out);
-                          });
-    });
-}
-
 }  // namespace cobalt

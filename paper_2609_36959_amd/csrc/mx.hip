@@ -1,5 +1,5 @@
 // Microscaled 4-bit rows: quantisation, and the experts' products on them.
-#include "forward.hpp"
+#include "few.hpp"
 
 namespace cobalt {
 namespace {

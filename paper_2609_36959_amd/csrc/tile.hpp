@@ -208,6 +208,19 @@ struct Bf16Math {
     }
 };
 
+// c + p q of 4-bit fragments of 128 k, a lane's 32 values (16 bytes) of each
+// times 2^(b - 127) with b byte kP of sp and byte kQ of sq.
+template <int kP, int kQ>
+__device__ __forceinline__ f32x4 mx_product(const bf16x8& p, const bf16x8& q, const f32x4& c,
+                                            int sp, int sq) {
+    typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+    constexpr int kFp4 = 4;  // E2M1 values, which take half of the operands' registers
+    const i32x4 a = __builtin_bit_cast(i32x4, p), b = __builtin_bit_cast(i32x4, q);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+        __builtin_shufflevector(a, a, 0, 1, 2, 3, -1, -1, -1, -1),
+        __builtin_shufflevector(b, b, 0, 1, 2, 3, -1, -1, -1, -1), c, kFp4, kFp4, kP, sp, kQ, sq);
+}
+
 // Products of 4-bit fragments: 128 k at a time, with the scales of both
 // operands. A lane's chunk of 16 bytes is one block of 32 values, so it needs
 // one scale byte of its row for each half of a step, and the two are
@@ -284,16 +297,9 @@ struct MxMath {
     }
     __device__ __forceinline__ f32x4 product(const bf16x8& pv, const bf16x8& qv, const f32x4& c,
                                              int x, int t, int kk) const {
-        typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
-        const i32x4 a4 = __builtin_bit_cast(i32x4, pv), b4 = __builtin_bit_cast(i32x4, qv);
-        // 4-bit operands take half of the registers
-        const auto a = __builtin_shufflevector(a4, a4, 0, 1, 2, 3, -1, -1, -1, -1);
-        const auto b = __builtin_shufflevector(b4, b4, 0, 1, 2, 3, -1, -1, -1, -1);
         // byte of the scales: half kk of an even or odd tile
         const auto mul = [&](auto bp, auto bq) {
-            constexpr int kFp4 = 4;
-            return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-                a, b, c, kFp4, kFp4, bp(), (int)sp[0][t / 2], bq(), (int)sq[0][x / 2]);
+            return mx_product<bp(), bq()>(pv, qv, c, (int)sp[0][t / 2], (int)sq[0][x / 2]);
         };
         const auto by_q = [&](auto bp) {
             const int n = kk + 2 * (x & 1);
@@ -428,17 +434,21 @@ __device__ __forceinline__ void start_rows(RowOperand<B, false, kWhole>& q, cons
     });
 }
 
-// Launches `kernel(b0, workgroups)` over ranges of the workgroups of mt x nt
-// tiles that a grid can hold.
+// Launches kernel(b0, n) over ranges [b0, b0 + n) of `all` workgroups that a
+// grid can hold.
 template <typename F>
-cobalt_status over_tiles(int64_t mt, int64_t nt, F&& kernel) {
-    const int64_t all = tile_grid(mt, nt), most = kMaxLaunchItems / 512 / 256 * 256;
+cobalt_status over_tiles(int64_t all, F&& kernel) {
+    const int64_t most = kMaxLaunchItems / 512 / 256 * 256;
     if (all > UINT32_MAX) return COBALT_EUNSUPPORTED;
     for (int64_t b0 = 0; b0 < all; b0 += most) {
         kernel((uint32_t)b0, (unsigned)std::min(all - b0, most));
         COBALT_LAUNCH_CHECK();
     }
     return COBALT_OK;
+}
+template <typename F>
+cobalt_status over_tiles(int64_t mt, int64_t nt, F&& kernel) {
+    return over_tiles(tile_grid(mt, nt), kernel);
 }
 
 // Calls f(TM) with the tiles' height for M places of E experts.
