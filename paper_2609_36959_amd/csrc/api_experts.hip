@@ -113,7 +113,7 @@ extern "C" cobalt_status cobalt_expert_down_backward(
     const Rows at{rows, out_rows};
     const hipStream_t s = (hipStream_t)stream;
     if (dw_down)
-        if (cobalt_status st = launch_weight_gradient(g, dout, d, true, h, f, false, at, dw_down,
+        if (cobalt_status st = launch_weight_gradient(g, dout, d, true, h, f, at, dw_down,
                                                       flags & COBALT_GRAD_FLOAT,
                                                       flags & COBALT_GRAD_ADD, ws, s))
             return st;
@@ -136,7 +136,7 @@ extern "C" cobalt_status cobalt_expert_gate_up_backward(
     const Rows at{rows, x_rows};
     const hipStream_t s = (hipStream_t)stream;
     if (dw_in)
-        if (cobalt_status st = launch_weight_gradient(g, dgate_up, 2 * f, false, x, d, true, at,
+        if (cobalt_status st = launch_weight_gradient(g, dgate_up, 2 * f, false, x, d, at,
                                                       dw_in, flags & COBALT_GRAD_FLOAT,
                                                       flags & COBALT_GRAD_ADD, ws, s))
             return st;

@@ -89,9 +89,10 @@ __device__ __forceinline__ bool find_tile(const Groups& g, int BM, uint32_t id, 
         lo = hi;
         hi = bound(e + 1);
     }
-    out->e = e;
-    out->lo = lo + (int)left * BM;
-    out->hi = min(hi, out->lo + BM);
+    // the same in every lane, which the compiler does not see
+    out->e = __builtin_amdgcn_readfirstlane(e);
+    out->lo = __builtin_amdgcn_readfirstlane(lo + (int)left * BM);
+    out->hi = min(__builtin_amdgcn_readfirstlane(hi), out->lo + BM);
     return true;
 }
 
@@ -109,10 +110,10 @@ cobalt_status launch_down_gradient(const Groups& g, const void* dout, Rows rows,
                                    void* dgate_up, hipStream_t s);
 cobalt_status launch_gate_up_gradient(const Groups& g, const void* dgate_up, int64_t d, int64_t f,
                                       const void* w_in, Rows rows, void* dx, hipStream_t s);
-// dw[e] (+)= sum_i a[i] b[i]^T over the places of e: a [.][na], b [.][nb],
-// taken at place i, or at its row where the flag says so.
+// dw[e] (+)= sum_i a[i] b[i]^T over the places of e: a [.][na], b [.][nb], the
+// one taken at place i, the other at its row (a_rows: a).
 cobalt_status launch_weight_gradient(const Groups& g, const void* a, int64_t na, bool a_rows,
-                                     const void* b, int64_t nb, bool b_rows, Rows rows, void* dw,
+                                     const void* b, int64_t nb, Rows rows, void* dw,
                                      bool f32, bool add, void* ws, hipStream_t s);
 size_t expert_backward_workspace_bytes(int64_t M, int E, int64_t d, int64_t f);
 

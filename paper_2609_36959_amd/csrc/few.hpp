@@ -15,6 +15,7 @@
 namespace cobalt {
 
 constexpr int kFewPlaces = 16;  // places of a tile
+constexpr int kFewWaves = 8;    // waves of a workgroup
 constexpr int kAhead = 4, kLeast = 8;
 
 // A lane's chunk of a fragment, with its scale where there are scales.
@@ -103,7 +104,7 @@ __device__ __forceinline__ void stream_products(float* sums, const Side& x, int6
             multiply(1, s + kAhead);
         }
     }
-    float* to = sums + ((part * (kWaves / KS) + wv / KS) * S) * 256 + i * 16 + g * 4;
+    float* to = sums + ((part * (kFewWaves / KS) + wv / KS) * S) * 256 + i * 16 + g * 4;
 #pragma unroll
     for (int k = 0; k < S; ++k) *(f32x4*)(to + k * 256) = acc[k];
     __syncthreads();
@@ -115,7 +116,7 @@ __device__ __forceinline__ float joined(const float* sums, int group, int k, int
     float v = 0.0f;
 #pragma unroll
     for (int part = 0; part < KS; ++part)
-        v += sums[((part * (kWaves / KS) + group) * S + k) * 256 + m * 16 + n];
+        v += sums[((part * (kFewWaves / KS) + group) * S + k) * 256 + m * 16 + n];
     return v;
 }
 
@@ -123,8 +124,8 @@ template <int KS, Act A, typename Side>
 __global__ __launch_bounds__(512) void gate_up_few_kernel(Groups g, uint32_t b0, Side x, Rows rows,
                                                           Side w, int64_t f, uint16_t* h,
                                                           uint16_t* gu) {
-    constexpr int kCols = 16 * (kWaves / KS);
-    __shared__ __attribute__((aligned(16))) float sums[kWaves * 2 * 256];
+    constexpr int kCols = 16 * (kFewWaves / KS);
+    __shared__ __attribute__((aligned(16))) float sums[kFewWaves * 2 * 256];
     const uint32_t nt = (uint32_t)((f + kCols - 1) / kCols), b = b0 + blockIdx.x;
     Tile t;
     if (!find_tile(g, kFewPlaces, b / nt, &t)) return;
@@ -150,8 +151,8 @@ __global__ __launch_bounds__(512) void gate_up_few_kernel(Groups g, uint32_t b0,
 template <int KS, typename Side>
 __global__ __launch_bounds__(512) void down_few_kernel(Groups g, uint32_t b0, Side h, Side w,
                                                        int64_t d, Rows rows, uint16_t* out) {
-    constexpr int kCols = 16 * (kWaves / KS);
-    __shared__ __attribute__((aligned(16))) float sums[kWaves * 256];
+    constexpr int kCols = 16 * (kFewWaves / KS);
+    __shared__ __attribute__((aligned(16))) float sums[kFewWaves * 256];
     const uint32_t nt = (uint32_t)((d + kCols - 1) / kCols), b = b0 + blockIdx.x;
     Tile t;
     if (!find_tile(g, kFewPlaces, b / nt, &t)) return;
@@ -183,7 +184,7 @@ inline bool few_rows(const Groups& g) { return g.M <= 16 * (int64_t)g.E; }
 
 // Workgroups for n columns.
 inline int64_t few_grid(const Groups& g, int64_t n, int ks) {
-    return most_tiles(g.M, g.E, kFewPlaces) * tiles(n, 16 * (kWaves / ks));
+    return most_tiles(g.M, g.E, kFewPlaces) * tiles(n, 16 * (kFewWaves / ks));
 }
 
 template <typename Side>
@@ -197,10 +198,11 @@ cobalt_status gate_up(const Groups& g, const Side& x, Rows rows, const Side& w, 
                         g, b0, x, rows, w, f, (uint16_t*)h, (uint16_t*)gu);
                 });
             });
-        return by_height(g, [&](auto tm) {
-            return over_tiles(most_tiles(g.M, g.E, tm * 32), tiles(f, kBN / 2),
+        return by_shape(g, f * 2, tiles(w.bytes, kStepBytes), [&](auto shape) {
+            typedef decltype(shape) S;
+            return over_tiles(most_tiles(g.M, g.E, S::kBM), tiles(f, S::kBN / 2),
                               [&](uint32_t b0, unsigned n) {
-                                  gate_up_kernel<tm(), a(), Side><<<n, 512, 0, s>>>(
+                                  gate_up_kernel<S, a(), Side><<<n, S::kThreads, 0, s>>>(
                                       g, b0, x, rows, w, f, (uint16_t*)h, (uint16_t*)gu);
                               });
         });
@@ -217,11 +219,12 @@ cobalt_status down(const Groups& g, const Side& h, const Side& w, int64_t d, Row
                     <<<n, 512, 0, s>>>(g, b0, h, w, d, rows, (uint16_t*)out);
             });
         });
-    return by_height(g, [&](auto tm) {
-        return over_tiles(most_tiles(g.M, g.E, tm * 32), tiles(d, kBN),
+    return by_shape(g, d, tiles(w.bytes, kStepBytes), [&](auto shape) {
+        typedef decltype(shape) S;
+        return over_tiles(most_tiles(g.M, g.E, S::kBM), tiles(d, S::kBN),
                           [&](uint32_t b0, unsigned n) {
-                              down_kernel<tm(), Side>
-                                  <<<n, 512, 0, s>>>(g, b0, h, w, d, rows, (uint16_t*)out);
+                              down_kernel<S, Side><<<n, S::kThreads, 0, s>>>(
+                                  g, b0, h, w, d, rows, (uint16_t*)out);
                           });
     });
 }

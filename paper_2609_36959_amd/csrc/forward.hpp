@@ -9,8 +9,8 @@ namespace cobalt {
 // Rows of `bytes` bytes at v; kWhole: whole steps.
 template <bool kW>
 struct Bf16Rows {
-    template <int TM>
-    using Math = Bf16Math<TM>;
+    template <typename S>
+    using Math = Bf16Math<S>;
     static constexpr bool kScaled = false, kWhole = kW;
     const char* v;
     int64_t bytes;
@@ -21,8 +21,8 @@ struct Bf16Rows {
 // Rows of `bytes` bytes of codes at v, `scales` bytes of scales at s.
 template <bool kW>
 struct MxRows {
-    template <int TM>
-    using Math = MxMath<TM, kW>;
+    template <typename S>
+    using Math = MxMath<S, kW>;
     static constexpr bool kScaled = true, kWhole = kW;
     const char* v;
     const char* s;
@@ -34,22 +34,22 @@ struct MxRows {
 };
 
 // A tile's operands: q row r is place lo + r's row of x; p row r is row
-// far(r) + near(r) of w, with far(r) the same for all rows of a wave's loads.
+// far(r) + near(r) of w, with far(r) the same for 32 neighbours.
 // A place without a row reads weights in its place, and its results are not
 // used.
-template <int TM, typename Side, typename F, typename G>
+template <typename S, typename Side, typename F, typename G>
 __device__ __forceinline__ void product_of_rows(char* lds, const Tile& t, const Side& x,
                                                 const Rows& rows, const Side& w, F&& far,
-                                                G&& near, Acc<TM>& acc) {
-    RowOperand<TM * 16 * kWM, false, Side::kWhole> q;
-    RowOperand<kBN, true, Side::kWhole> p;
-    typename Side::template Math<TM> math;
+                                                G&& near, Acc<S::kTM>& acc) {
+    RowOperand<S, S::kBM, false, Side::kWhole> q;
+    RowOperand<S, S::kBN, true, Side::kWhole> p;
+    typename Side::template Math<S> math;
     const auto place = [&](int r) { return rows.of(min(t.lo + r, t.hi - 1)); };
-    q.start(x.bytes, nullptr, [&](int r) {
+    q.start(x.bytes, 0, [&](int r) {
         const int64_t at = place(r);
         return at < 0 ? w.row(far(0)) : x.row(at);
     });
-    p.start(w.bytes, w.row(far(wave_id() * 8)),
+    p.start(w.bytes, [&](int r) { return w.row(far(r)); },
             [&](int r) { return (uint32_t)near(r) * (uint32_t)w.bytes; });
     if constexpr (Side::kScaled)
         math.start(
@@ -60,28 +60,27 @@ __device__ __forceinline__ void product_of_rows(char* lds, const Tile& t, const 
             },
             w.scale_row(far(wave_id() * 32)),
             [&](int r) { return (uint32_t)near(r) * (uint32_t)w.scales; });
-    multiply<TM>(lds, q, p, math, (int)((x.bytes + kStepBytes - 1) / kStepBytes), acc);
+    multiply<S>(lds, q, p, math, (int)((x.bytes + kStepBytes - 1) / kStepBytes), acc);
 }
 
 // h = act(gate) * up. The weight rows of a tile: a wave's 64 are 32 gate rows
 // and the 32 up rows of the same columns, in the order that gives a lane eight
 // consecutive columns of both, so that the product needs no other lane.
-template <int TM, Act A, typename Side>
-__global__ __launch_bounds__(512) void gate_up_kernel(Groups g, uint32_t b0, Side x, Rows rows,
+template <typename S, Act A, typename Side>
+__global__ __launch_bounds__(S::kThreads) void gate_up_kernel(Groups g, uint32_t b0, Side x, Rows rows,
                                                       Side w, int64_t f, uint16_t* h,
                                                       uint16_t* gu) {
-    constexpr int kBM = TM * 16 * kWM;
+    constexpr int TM = S::kTM, kBM = S::kBM, kBN = S::kBN, kWN = S::kWN;
     __shared__
-        __attribute__((aligned(1024))) char lds[tile_lds<TM, typename Side::template Math<TM>>()];
+        __attribute__((aligned(1024))) char lds[tile_lds<S, typename Side::template Math<S>>()];
     const TileAt at = tile_at(b0 + blockIdx.x, (uint32_t)((f + kBN / 2 - 1) / (kBN / 2)));
     Tile t;
     if (!find_tile(g, kBM, at.m, &t)) return;
     const int64_t n0 = (int64_t)at.n * (kBN / 2);
     Acc<TM> acc;
     const int last = (int)min(f - 1 - n0, (int64_t)kBN);
-    // row r is an up row where r / 32 is odd: a wave loads eight rows of every
-    // 64, or the scales of 32
-    product_of_rows<TM>(
+    // row r is an up row where r / 32 is odd
+    product_of_rows<S>(
         lds, t, x, rows, w,
         [&](int r) { return ((int64_t)t.e * 2 + ((r >> 5) & 1)) * f + n0; },
         [&](int r) {
@@ -113,19 +112,19 @@ __global__ __launch_bounds__(512) void gate_up_kernel(Groups g, uint32_t b0, Sid
 
 // out = w h. The order of a wave's 64 weight rows gives a lane sixteen
 // consecutive columns.
-template <int TM, typename Side>
-__global__ __launch_bounds__(512) void down_kernel(Groups g, uint32_t b0, Side h, Side w,
+template <typename S, typename Side>
+__global__ __launch_bounds__(S::kThreads) void down_kernel(Groups g, uint32_t b0, Side h, Side w,
                                                    int64_t d, Rows rows, uint16_t* out) {
-    constexpr int kBM = TM * 16 * kWM;
+    constexpr int TM = S::kTM, kBM = S::kBM, kBN = S::kBN, kWN = S::kWN;
     __shared__
-        __attribute__((aligned(1024))) char lds[tile_lds<TM, typename Side::template Math<TM>>()];
+        __attribute__((aligned(1024))) char lds[tile_lds<S, typename Side::template Math<S>>()];
     const TileAt at = tile_at(b0 + blockIdx.x, (uint32_t)((d + kBN - 1) / kBN));
     Tile t;
     if (!find_tile(g, kBM, at.m, &t)) return;
     const int64_t n0 = (int64_t)at.n * kBN;
     Acc<TM> acc;
     const int last = (int)min(d - 1 - n0, (int64_t)kBN);
-    product_of_rows<TM>(
+    product_of_rows<S>(
         lds, t, h, Rows{nullptr, g.M}, w,
         [&](int) { return t.e * d + n0; },
         [&](int r) {

@@ -29,8 +29,14 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef int16_t s16x4 __attribute__((ext_vector_type(4)));
 typedef int16_t s16x8 __attribute__((ext_vector_type(8)));
 
-constexpr int kWaves = 8, kWM = 2, kWN = 4;  // waves of a workgroup, along m and n
-constexpr int kBN = 256;
+// A tile of kBM x kBN results made by kWM x kWN waves, each with TM x 4 tiles
+// of 16 x 16.
+template <int WN, int TM>
+struct Shape {
+    static constexpr int kWM = 2, kWN = WN, kTM = TM;
+    static constexpr int kWaves = kWM * kWN, kThreads = 64 * kWaves;
+    static constexpr int kBM = kWM * TM * 16, kBN = kWN * 64;
+};
 constexpr int kStepBytes = 128;
 
 // What is loaded for k past the end, on both sides of a product.
@@ -53,14 +59,14 @@ __device__ __forceinline__ int wave_id() {
 // kWhole: the rows are whole steps, and no load has to look for their end.
 // kNear: the rows lie within 4 GiB from an address that is the same for a whole
 // wave, and a lane keeps 32-bit offsets; otherwise they are anywhere.
-template <int B, bool kNear, bool kWhole>
+template <typename S, int B, bool kNear, bool kWhole>
 struct RowOperand {
     static constexpr bool kColumns = false;
-    static constexpr int kLoads = B / 8 / kWaves;
+    static constexpr int kWaves = S::kWaves, kLoads = B / 8 / kWaves;
     static constexpr int kReads = 1;  // LDS reads per fragment
     typedef std::conditional_t<kNear, uint32_t, const char*> At;
     At p[kLoads];
-    const char* base;
+    const char* base[kLoads];
     int64_t bytes;
 
     __device__ __forceinline__ static int row_of(int j) {
@@ -70,17 +76,20 @@ struct RowOperand {
     __device__ __forceinline__ static int chunk() {
         return (threadIdx.x & 7) ^ ((row_of(0) >> 1) & 7);
     }
-    // row(r): row r of the tile, as an offset from `first` or an address
-    template <typename F>
-    __device__ __forceinline__ void start(int64_t row_bytes, const char* first, F&& row) {
+    // row(r): row r of the tile, as an address, or as an offset from first(r8)
+    // with r8 = r / 8 * 8
+    template <typename F, typename R>
+    __device__ __forceinline__ void start(int64_t row_bytes, F&& first, R&& row) {
         bytes = row_bytes;
-        base = first;
 #pragma unroll
-        for (int j = 0; j < kLoads; ++j) p[j] = (At)row(row_of(j)) + chunk() * 16;
+        for (int j = 0; j < kLoads; ++j) {
+            if constexpr (kNear) base[j] = first((j * kWaves + wave_id()) * 8);
+            p[j] = (At)row(row_of(j)) + chunk() * 16;
+        }
     }
     __device__ __forceinline__ const char* at(int j) const {
         if constexpr (kNear)
-            return base + p[j];
+            return base[j] + p[j];
         else
             return p[j];
     }
@@ -95,11 +104,12 @@ struct RowOperand {
                 *(u32x4*)(lds + (j * kWaves + w) * 1024 + (threadIdx.x & 63) * 16) =
                     u32x4{0, 0, 0, 0};
         }
-        if constexpr (kNear) {
-            base += kStepBytes;
-        } else {
 #pragma unroll
-            for (int j = 0; j < kLoads; ++j) p[j] += kStepBytes;
+        for (int j = 0; j < kLoads; ++j) {
+            if constexpr (kNear)
+                base[j] += kStepBytes;
+            else
+                p[j] += kStepBytes;
         }
     }
     // The wave's part of rows r0 + 16 t + (0..15) for half kk of the step: a
@@ -114,49 +124,57 @@ struct RowOperand {
 // A bf16 operand whose k runs over the rows of memory, B consecutive values of
 // each: 64 rows of 2B bytes in LDS for one step. Lanes get eight consecutive k
 // of their column by two transposing reads of four rows each. The 32-byte
-// unit u of row k lies at unit u ^ (k % 4 + k / 16 % 2 * 4): a half wave reads
-// one unit of eight rows, from eight different groups of eight banks.
-// kWhole: k is a multiple of a step and the rows have no index.
-template <int B, bool kWhole>
+// units of row k are exchanged by place(k), so that the units that a half wave
+// reads, one of each of eight rows, lie in eight different groups of banks.
+// kWhole: k is a multiple of a step. kGather: row k is row idx[k] of the
+// n_rows in memory, and zero where there is no such row.
+template <typename S, int B, bool kWhole, bool kGather>
 struct ColumnOperand {
     static constexpr bool kColumns = true;
     static constexpr int kRowBytes = 2 * B;
-    static constexpr int kLoads = B * 128 / 1024 / kWaves;
+    static constexpr int kWaves = S::kWaves, kLoads = B * 128 / 1024 / kWaves;
     static constexpr int kReads = 2;
-    const char* base;   // first column of the tile, in row 0
-    int64_t pitch;      // bytes between rows
-    int64_t rows;       // k
-    const int32_t* idx; // row of each k, or NULL
-    int64_t n_rows;
-    int32_t next[kLoads];  // idx of the rows of the step to come
-    uint32_t at[kLoads];   // the lane's chunk: byte in the row, or in the step (kWhole)
+    const char* base;  // first column of the tile, in row 0 or in the step's first row
+    int64_t pitch;     // bytes between rows
+    int rows;          // k
+    const int32_t* idx;
+    uint32_t n_rows;
+    uint32_t at[kLoads];    // byte of the lane's chunk in the row (kGather) or the step
+    uint32_t next[kLoads];  // rows of the step to come (kGather)
 
+    // bit0, bit1: bits 0 and 1 of k; bit4: its bit 4
+    __device__ __forceinline__ static int place(int bit0, int bit1, int bit4) {
+        // rows of 128 bytes: even and odd ones lie in different banks already
+        return B == 64 ? bit1 | bit4 << 1 : bit0 | bit1 << 1 | bit4 << 2;
+    }
     __device__ __forceinline__ static int row_of(int j) {
         return (j * kWaves + wave_id()) * (1024 / kRowBytes) + (threadIdx.x & 63) * 16 / kRowBytes;
     }
-    // cols: columns of the tile that there are (a multiple of 8)
-    __device__ void start(const void* first, int64_t cols, int64_t row_bytes, int64_t k,
-                          const int32_t* index, int64_t index_rows) {
+    // cols: columns from `first` on that there are (a multiple of 8)
+    __device__ __forceinline__ void start(const void* first, int64_t cols, int64_t row_bytes,
+                                          int k, const int32_t* index, int64_t index_rows) {
         const int lane = threadIdx.x & 63;
         base = (const char*)first;
         pitch = row_bytes;
         rows = k;
         idx = index;
-        n_rows = index_rows;
-        if (!kWhole && idx) fetch(0);
+        n_rows = (uint32_t)min(index_rows, int64_t(1) << 31);
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
             const int r = row_of(j), slot = lane * 16 % kRowBytes / 16;
-            const int unit = (slot >> 1) ^ ((r & 3) | (((r >> 4) & 1) << 2));
+            const int unit = (slot >> 1) ^ place(r & 1, (r >> 1) & 1, (r >> 4) & 1);
             const int c = (unit * 2 + (slot & 1)) * 8;
-            at[j] = (c < cols ? c : (int)cols - 8) * 2 + (kWhole ? r * (uint32_t)pitch : 0);
+            at[j] = (c < cols ? c : (int)cols - 8) * 2 + (kGather ? 0 : r * (uint32_t)pitch);
         }
+        if (kGather) fetch(0);
     }
+    // the rows of step s; behind the last k, none
     __device__ __forceinline__ void fetch(int s) {
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
-            const int64_t k = (int64_t)s * 64 + row_of(j);
-            next[j] = idx[k < rows ? k : rows - 1];
+            const int k = s * 64 + row_of(j);
+            const int r = idx[min(k, rows - 1)];
+            next[j] = k < rows ? (uint32_t)r : ~0u;
         }
     }
     __device__ __forceinline__ void load(char* lds, int s) {
@@ -164,23 +182,22 @@ struct ColumnOperand {
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
             char* to = lds + (j * kWaves + w) * 1024;
-            if constexpr (kWhole) {
-                load_to_lds(base + at[j], to);
+            if constexpr (kGather) {
+                const char* p = base + at[j] + (uint64_t)next[j] * (uint32_t)pitch;
+                load_to_lds(next[j] < n_rows ? p : (const char*)kNothing, to);
             } else {
-                const int64_t k = (int64_t)s * 64 + row_of(j);
-                const int64_t r = idx ? next[j] : k;
-                const bool ok = k < rows && r >= 0 && r < n_rows;
-                load_to_lds(ok ? base + r * pitch + at[j] : (const char*)kNothing, to);
+                const char* p = base + at[j];
+                load_to_lds(kWhole || s * 64 + row_of(j) < rows ? p : (const char*)kNothing, to);
             }
         }
-        if constexpr (kWhole)
-            base += 64 * pitch;
-        else if (idx)
+        if constexpr (kGather)
             fetch(s + 1);
+        else
+            base += 64 * pitch;
     }
     __device__ __forceinline__ static bf16x8 read(const char* lds, int c0, int t, int kk) {
         const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
-        const int unit = (c0 / 16 + t) ^ ((i >> 2) | ((g & 1) << 2));
+        const int unit = (c0 / 16 + t) ^ place((i >> 2) & 1, i >> 3, g & 1);
         const char* a = lds + (16 * g + 8 * kk + (i >> 2)) * kRowBytes + unit * 32 + (i & 3) * 8;
         typedef __attribute__((address_space(3))) s16x4* lds4;
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)a);
@@ -195,7 +212,7 @@ template <int TM>
 using Acc = f32x4[TM][4];
 
 // Products of bf16 fragments: 32 k at a time.
-template <int TM>
+template <typename S>
 struct Bf16Math {
     static constexpr int kLds = 0, kReads = 0;
     __device__ __forceinline__ void prefetch(int) {}
@@ -228,9 +245,10 @@ __device__ __forceinline__ f32x4 mx_product(const bf16x8& p, const bf16x8& q, co
 // (rows of scales need not be aligned) into LDS, one dword per thread and
 // operand. There the two bytes of row r and chunk pair g lie next to those of
 // row r + 16 (r % 32 < 16), so that one dword serves a lane for two tiles.
-template <int TM, bool kWhole>
+template <typename S, bool kWhole>
 struct MxMath {
-    static constexpr int kBM = TM * 16 * kWM;
+    static constexpr int TM = S::kTM, kBM = S::kBM, kBN = S::kBN;
+    static_assert(kBN * 2 == S::kThreads && kBM <= kBN, "a dword per thread and operand");
     static constexpr int kLds = 2 * (kBM + kBN) * 8, kReads = TM / 2 + 2;
     const char* q;     // scales of the thread's row of q, at its dword of the step
     const char* base;  // of the row of p: at a 32-bit offset from here
@@ -261,7 +279,7 @@ struct MxMath {
         return v;
     }
     __device__ __forceinline__ void prefetch(int) {
-        if (kBM == 256 || threadIdx.x < kBM * 2) next_q = dword(q, left);
+        if (kBM == kBN || threadIdx.x < kBM * 2) next_q = dword(q, left);
         next_p = dword(base + p, left);
         q += 8;
         base += 8;
@@ -275,15 +293,15 @@ struct MxMath {
     }
     __device__ __forceinline__ void commit(char* lds, int s) {
         char* to = lds + (s & 1) * (kLds / 2);
-        if (kBM == 256 || threadIdx.x < kBM * 2) put(to, next_q);
+        if (kBM == kBN || threadIdx.x < kBM * 2) put(to, next_q);
         put(to + kBM * 8, next_p);
     }
     // the scales of step s, for both halves
     __device__ __forceinline__ void read(const char* lds, int s) {
         const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4, w = wave_id();
         const char* at = lds + (s & 1) * (kLds / 2) + i * 16 + g * 4;
-        const char* aq = at + w / kWN * (TM * 16) * 8;
-        const char* ap = at + (kBM + w % kWN * 64) * 8;
+        const char* aq = at + w / S::kWN * (TM * 16) * 8;
+        const char* ap = at + (kBM + w % S::kWN * 64) * 8;
 #pragma unroll
         for (int t = 0; t < TM / 2; ++t) sq[1][t] = *(const uint32_t*)(aq + t * 256);
 #pragma unroll
@@ -317,16 +335,16 @@ struct MxMath {
 };
 
 // LDS of a tile: two stages, and what the products need besides.
-template <int TM, typename Math>
+template <typename S, typename Math>
 constexpr size_t tile_lds() {
-    return 2 * (size_t)(TM * 16 * kWM + kBN) * kStepBytes + Math::kLds;
+    return 2 * (size_t)(S::kBM + S::kBN) * kStepBytes + Math::kLds;
 }
 
-template <int TM, typename Q, typename P, typename Math>
+template <typename S, typename Q, typename P, typename Math>
 __device__ __forceinline__ void multiply(char* lds, Q& q, P& p, Math& math, int steps,
-                                         Acc<TM>& acc) {
-    constexpr int kBM = TM * 16 * kWM, kStage = (kBM + kBN) * kStepBytes;
-    const int w = wave_id(), m0 = w / kWN * (TM * 16), n0 = w % kWN * 64;
+                                         Acc<S::kTM>& acc) {
+    constexpr int TM = S::kTM, kBM = S::kBM, kStage = (kBM + S::kBN) * kStepBytes;
+    const int w = wave_id(), m0 = w / S::kWN * (TM * 16), n0 = w % S::kWN * 64;
     char* extra = lds + 2 * kStage;
     bf16x8 fq[2][TM], fp[2][4];
     const auto load = [&](int s) {
@@ -392,6 +410,30 @@ __device__ __forceinline__ void multiply(char* lds, Q& q, P& p, Math& math, int 
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
+// Calls store(m, n, v) for the results of a tile after multiply(), eight
+// consecutive n (n % 8 == 0) per lane and whole 128-byte lines of n per
+// instruction: each wave turns its results in LDS, 16 rows of m at a time.
+template <typename S, typename F>
+__device__ __forceinline__ void store_rows(char* lds, const Acc<S::kTM>& acc, F&& store) {
+    constexpr int kPitch = 64 + 4;  // floats: rows shifted by four banks
+    const int lane = threadIdx.x & 63, w = wave_id();
+    float* part = (float*)lds + w * 16 * kPitch;
+    const int m0 = w / S::kWN * (S::kTM * 16), n0 = w % S::kWN * 64;
+#pragma unroll
+    for (int y = 0; y < S::kTM; ++y) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            *(f32x4*)(part + (lane & 15) * kPitch + k * 16 + (lane >> 4) * 4) = acc[y][k];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int m = half * 8 + lane / 8, n = lane % 8 * 8;
+            const f32x4 v[2] = {*(const f32x4*)(part + m * kPitch + n),
+                                *(const f32x4*)(part + m * kPitch + n + 4)};
+            store(m0 + y * 16 + m, n0 + n, v);
+        }
+    }
+}
+
 // The tile of workgroup b among mt x nt tiles. Eight consecutive workgroups
 // run on eight XCDs; of every 256, each XCD takes 32 consecutive tiles, and
 // those are four rows of tiles by eight columns, so that what they load meets
@@ -425,17 +467,17 @@ __device__ __forceinline__ u32x2 pack4(const f32x4& a) {
 
 // Places [lo, hi) of a tile as rows of x for the operand q: a place without a
 // row reads `other`, any row of the same length, and its results are not used.
-template <int B, bool kWhole>
-__device__ __forceinline__ void start_rows(RowOperand<B, false, kWhole>& q, const Tile& t, const char* x,
+template <typename S, int B, bool kWhole>
+__device__ __forceinline__ void start_rows(RowOperand<S, B, false, kWhole>& q, const Tile& t, const char* x,
                                            const Rows& rows, const char* other, int64_t bytes) {
-    q.start(bytes, nullptr, [&](int r) {
+    q.start(bytes, 0, [&](int r) {
         const int64_t at = rows.of(min(t.lo + r, t.hi - 1));
         return at < 0 ? other : x + at * bytes;
     });
 }
 
-// Launches kernel(b0, n) over ranges [b0, b0 + n) of `all` workgroups that a
-// grid can hold.
+// Launches kernel(b0, n) over ranges [b0, b0 + n) of `all` workgroups of at
+// most 512 threads that a grid can hold.
 template <typename F>
 cobalt_status over_tiles(int64_t all, F&& kernel) {
     const int64_t most = kMaxLaunchItems / 512 / 256 * 256;
@@ -451,13 +493,14 @@ cobalt_status over_tiles(int64_t mt, int64_t nt, F&& kernel) {
     return over_tiles(tile_grid(mt, nt), kernel);
 }
 
-// Calls f(TM) with the tiles' height for M places of E experts.
+// Calls f(shape) with the tiles for M places of E experts, n columns and
+// `steps` steps of k.
 template <typename F>
-cobalt_status by_height(const Groups& g, F&& f) {
+cobalt_status by_shape(const Groups& g, int64_t n, int64_t steps, F&& f) {
     const int64_t mean = g.M / g.E;
-    if (mean <= 64) return f(std::integral_constant<int, 2>());
-    if (mean <= 128) return f(std::integral_constant<int, 4>());
-    return f(std::integral_constant<int, 8>());
+    if (mean <= 64) return f(Shape<4, 2>());
+    if (mean <= 128) return f(Shape<4, 4>());
+    return f(Shape<4, 8>());
 }
 
 // Calls f(act) with the activation as a constant.
