@@ -4,107 +4,135 @@
 namespace cobalt {
 namespace {
 
-template <typename S, Act A, bool kWhole>
-__global__ __launch_bounds__(S::kThreads) void down_gradient_kernel(Groups g, uint32_t b0,
-                                                            const char* dout, Rows rows, int64_t d,
-                                                            int64_t f, const char* w,
-                                                            const uint16_t* gu, uint16_t* dgu) {
-    constexpr int TM = S::kTM, kBM = S::kBM, kBN = S::kBN, kWN = S::kWN;
-    __shared__ __attribute__((aligned(1024))) char lds[tile_lds<S, Bf16Math<S>>()];
-    const TileAt at = tile_at(b0 + blockIdx.x, (uint32_t)((f + kBN - 1) / kBN));
-    Tile t;
-    if (!find_tile(g, kBM, at.m, &t)) return;
-    const int64_t n0 = (int64_t)at.n * kBN;
-    const char* we = w + (int64_t)t.e * d * f * 2;
-    RowOperand<S, kBM, false, kWhole> q;
-    ColumnOperand<S, kBN, kWhole, false> p;
-    start_rows(q, t, dout, rows, we, d * 2);
-    p.start(we + n0 * 2, f - n0, f * 2, (int)d, nullptr, 0);
-    Acc<TM> acc;
-    Bf16Math<S> math;
-    multiply<S>(lds, q, p, math, (int)((d * 2 + kStepBytes - 1) / kStepBytes), acc);
-    store_rows<S>(lds, acc, [&](int m, int c, const f32x4 (&v)[2]) {
-        const int64_t i = t.lo + m, n = n0 + c;
-        if (i >= t.hi || n >= f) return;
-        const bool ok = rows.of(i) >= 0;
-        const u32x4 gb = *(const u32x4*)(gu + i * 2 * f + n);
-        const u32x4 ub = *(const u32x4*)(gu + i * 2 * f + f + n);
-        f32x4 dg[2], du[2];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const float gv = k & 1 ? high(gb[k / 2]) : low(gb[k / 2]);
-            const float uv = k & 1 ? high(ub[k / 2]) : low(ub[k / 2]);
-            const float dh = ok ? v[k / 4][k % 4] : 0.0f;
-            dg[k / 4][k % 4] = dh * uv * act_slope<A>(gv);
-            du[k / 4][k % 4] = dh * act<A>(gv);
-        }
-        *(u32x4*)(dgu + i * 2 * f + n) = pack8(dg[0], dg[1]);
-        *(u32x4*)(dgu + i * 2 * f + f + n) = pack8(du[0], du[1]);
-    });
-}
-
+// The steps of a tile of rows and of weights whose rows are k.
 template <typename S, bool kWhole>
-__global__ __launch_bounds__(S::kThreads) void gate_up_gradient_kernel(Groups g, uint32_t b0,
-                                                               const char* dgu, int64_t d,
-                                                               int64_t f, const char* w, Rows rows,
-                                                               uint16_t* dx) {
-    constexpr int TM = S::kTM, kBM = S::kBM, kBN = S::kBN, kWN = S::kWN;
-    __shared__ __attribute__((aligned(1024))) char lds[tile_lds<S, Bf16Math<S>>()];
-    const TileAt at = tile_at(b0 + blockIdx.x, (uint32_t)((d + kBN - 1) / kBN));
-    Tile t;
-    if (!find_tile(g, kBM, at.m, &t)) return;
-    const int64_t n0 = (int64_t)at.n * kBN;
-    const char* we = w + (int64_t)t.e * 2 * f * d * 2;
-    RowOperand<S, kBM, false, kWhole> q;
-    ColumnOperand<S, kBN, kWhole, false> p;
-    start_rows(q, t, dgu, Rows{nullptr, g.M}, we, f * 4);
-    p.start(we + n0 * 2, d - n0, d * 2, (int)(2 * f), nullptr, 0);
-    Acc<TM> acc;
-    Bf16Math<S> math;
-    multiply<S>(lds, q, p, math, (int)((f * 4 + kStepBytes - 1) / kStepBytes), acc);
-    store_rows<S>(lds, acc, [&](int m, int c, const f32x4 (&v)[2]) {
-        const int64_t i = t.lo + m, n = n0 + c;
-        if (i >= t.hi || n >= d) return;
-        const int64_t r = rows.of(i);
-        if (r >= 0) *(u32x4*)(dx + r * d + n) = pack8(v[0], v[1]);
-    });
+using TurnedPipe = Pipe<S, RowOperand<S, S::kBM, false, kWhole>,
+                        ColumnOperand<S, S::kBN, kWhole, false>, Bf16Math<S>>;
+
+// dh = w^T dout, and through the product and the activation.
+template <typename S, Act A, bool kWhole>
+__global__ __launch_bounds__(S::kThreads, 2) void down_gradient_kernel(
+    Groups g, uint32_t b0, uint32_t all, const char* dout, Rows rows, int64_t d, int64_t f,
+    const char* w, const uint16_t* gu, uint16_t* dgu) {
+    constexpr int kBN = S::kBN;
+    typedef Lds<S, Bf16Math<S>, true> L;
+    __shared__ __attribute__((aligned(1024))) char lds[L::kBytes];
+    TurnedPipe<S, kWhole> pipe;
+    pipe.lds = lds;
+    make_tiles<S, RowJob>(
+        pipe, b0 + blockIdx.x, all,
+        [&](uint32_t b, RowJob* job) {
+            job->steps = (int)((d * 2 + kStepBytes - 1) / kStepBytes);
+            return find_rows<S>(g, b, (uint32_t)((f + kBN - 1) / kBN), kBN, job);
+        },
+        [&](const RowJob& job) {
+            const char* we = w + (int64_t)job.t.e * d * f * 2;
+            start_rows(pipe.q, job.t, dout, rows, we, d * 2);
+            pipe.p.start(we + job.n0 * 2, f - job.n0, f * 2, (int)d, nullptr, 0);
+        },
+        [&](const RowJob& job, const Acc<S::kTM>& acc) {
+            store_rows<S>(L::turn(lds), acc, [&](int m, int c, const f32x4 (&v)[2]) {
+                const int64_t i = job.t.lo + m, n = job.n0 + c;
+                if (i >= job.t.hi || n >= f) return;
+                const bool ok = rows.of(i) >= 0;
+                const u32x4 gb = *(const u32x4*)(gu + i * 2 * f + n);
+                const u32x4 ub = *(const u32x4*)(gu + i * 2 * f + f + n);
+                f32x4 dg[2], du[2];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const float gv = k & 1 ? high(gb[k / 2]) : low(gb[k / 2]);
+                    const float uv = k & 1 ? high(ub[k / 2]) : low(ub[k / 2]);
+                    const float dh = ok ? v[k / 4][k % 4] : 0.0f;
+                    dg[k / 4][k % 4] = dh * uv * act_slope<A>(gv);
+                    du[k / 4][k % 4] = dh * act<A>(gv);
+                }
+                *(u32x4*)(dgu + i * 2 * f + n) = pack8(dg[0], dg[1]);
+                *(u32x4*)(dgu + i * 2 * f + f + n) = pack8(du[0], du[1]);
+            });
+        });
 }
 
-// Tiles of all experts' gradients, expert by expert.
+// dx = w^T (dgate, dup).
+template <typename S, bool kWhole>
+__global__ __launch_bounds__(S::kThreads, 2) void gate_up_gradient_kernel(
+    Groups g, uint32_t b0, uint32_t all, const char* dgu, int64_t d, int64_t f, const char* w,
+    Rows rows, uint16_t* dx) {
+    constexpr int kBN = S::kBN;
+    typedef Lds<S, Bf16Math<S>, true> L;
+    __shared__ __attribute__((aligned(1024))) char lds[L::kBytes];
+    TurnedPipe<S, kWhole> pipe;
+    pipe.lds = lds;
+    make_tiles<S, RowJob>(
+        pipe, b0 + blockIdx.x, all,
+        [&](uint32_t b, RowJob* job) {
+            job->steps = (int)((f * 4 + kStepBytes - 1) / kStepBytes);
+            return find_rows<S>(g, b, (uint32_t)((d + kBN - 1) / kBN), kBN, job);
+        },
+        [&](const RowJob& job) {
+            const char* we = w + (int64_t)job.t.e * 2 * f * d * 2;
+            start_rows(pipe.q, job.t, dgu, Rows{nullptr, g.M}, we, f * 4);
+            pipe.p.start(we + job.n0 * 2, d - job.n0, d * 2, (int)(2 * f), nullptr, 0);
+        },
+        [&](const RowJob& job, const Acc<S::kTM>& acc) {
+            store_rows<S>(L::turn(lds), acc, [&](int m, int c, const f32x4 (&v)[2]) {
+                const int64_t i = job.t.lo + m, n = job.n0 + c;
+                if (i >= job.t.hi || n >= d) return;
+                const int64_t r = rows.of(i);
+                if (r >= 0) *(u32x4*)(dx + r * d + n) = pack8(v[0], v[1]);
+            });
+        });
+}
+
+// Tiles of all experts' gradients, expert by expert; mt: tiles along m of one.
+struct GradJob {
+    int64_t m0, n0;
+    int e, lo, hi, steps;
+};
 template <typename S, bool kFloat, bool kAdd, bool kGatherA, bool kGatherB>
-__global__ __launch_bounds__(S::kThreads) void weight_gradient_kernel(
-    Groups g, uint32_t b0, uint32_t mt, const char* a, int64_t na, const char* b, int64_t nb,
-    Rows rows, void* dw) {
-    constexpr int TM = S::kTM, kBM = S::kBM, kBN = S::kBN;
-    __shared__ __attribute__((aligned(1024))) char lds[tile_lds<S, Bf16Math<S>>()];
-    const TileAt at = tile_at(b0 + blockIdx.x, (uint32_t)((nb + kBN - 1) / kBN));
-    const uint32_t e = at.m / mt;
-    if (e >= (uint32_t)g.E) return;
-    const int64_t m0 = (int64_t)(at.m % mt) * kBM, n0 = (int64_t)at.n * kBN;
-    const int lo = min(max(g.off[e], 0), g.M), hi = min(max(g.off[e + 1], 0), g.M);
-    Acc<TM> acc = {};
-    if (hi > lo) {
-        ColumnOperand<S, kBM, false, kGatherA> q;
-        ColumnOperand<S, kBN, false, kGatherB> p;
-        Bf16Math<S> math;
-        q.start(a + (kGatherA ? 0 : lo * na * 2) + m0 * 2, na - m0, na * 2, hi - lo,
-                rows.idx + lo, rows.n);
-        p.start(b + (kGatherB ? 0 : lo * nb * 2) + n0 * 2, nb - n0, nb * 2, hi - lo,
-                rows.idx + lo, rows.n);
-        multiply<S>(lds, q, p, math, (hi - lo + 63) / 64, acc);
-    }
-    store_rows<S>(lds, acc, [&](int r, int c, const f32x4 (&v)[2]) {
-        const int64_t m = m0 + r, n = n0 + c;
-        if (m >= na || n >= nb) return;
-        const int64_t i = ((int64_t)e * na + m) * nb + n;
-        if constexpr (!kFloat) {
-            *(u32x4*)((uint16_t*)dw + i) = pack8(v[0], v[1]);
-        } else {
-            f32x4* to = (f32x4*)((float*)dw + i);
-            to[0] = kAdd ? to[0] + v[0] : v[0];
-            to[1] = kAdd ? to[1] + v[1] : v[1];
-        }
-    });
+__global__ __launch_bounds__(S::kThreads, 2) void weight_gradient_kernel(
+    Groups g, uint32_t b0, uint32_t all, uint32_t mt, const char* a, int64_t na, const char* b,
+    int64_t nb, Rows rows, void* dw) {
+    constexpr int kBM = S::kBM, kBN = S::kBN;
+    typedef Lds<S, Bf16Math<S>, true> L;
+    __shared__ __attribute__((aligned(1024))) char lds[L::kBytes];
+    Pipe<S, ColumnOperand<S, kBM, false, kGatherA>, ColumnOperand<S, kBN, false, kGatherB>,
+         Bf16Math<S>>
+        pipe;
+    pipe.lds = lds;
+    make_tiles<S, GradJob>(
+        pipe, b0 + blockIdx.x, all,
+        [&](uint32_t id, GradJob* job) {
+            const TileAt at = tile_at(id, (uint32_t)((nb + kBN - 1) / kBN));
+            if (at.m / kBand * kBand >= mt * (uint32_t)g.E) return -1;
+            const int e = (int)(at.m / mt);
+            if (e >= g.E) return 0;
+            const int lo = min(max(g.off[e], 0), g.M), hi = min(max(g.off[e + 1], 0), g.M);
+            *job = {(int64_t)(at.m % mt) * kBM, (int64_t)at.n * kBN, e, lo, hi,
+                    hi > lo ? (hi - lo + 63) / 64 : 0};
+            return 1;
+        },
+        [&](const GradJob& job) {
+            if (job.steps == 0) return;
+            const int lo = job.lo, k = job.hi - lo;
+            pipe.q.start(a + (kGatherA ? 0 : lo * na * 2) + job.m0 * 2, na - job.m0, na * 2, k,
+                         rows.idx + lo, rows.n);
+            pipe.p.start(b + (kGatherB ? 0 : lo * nb * 2) + job.n0 * 2, nb - job.n0, nb * 2, k,
+                         rows.idx + lo, rows.n);
+        },
+        [&](const GradJob& job, const Acc<S::kTM>& acc) {
+            store_rows<S>(L::turn(lds), acc, [&](int r, int c, const f32x4 (&v)[2]) {
+                const int64_t m = job.m0 + r, n = job.n0 + c;
+                if (m >= na || n >= nb) return;
+                const int64_t i = ((int64_t)job.e * na + m) * nb + n;
+                if constexpr (!kFloat) {
+                    *(u32x4*)((uint16_t*)dw + i) = pack8(v[0], v[1]);
+                } else {
+                    f32x4* to = (f32x4*)((float*)dw + i);
+                    to[0] = kAdd ? to[0] + v[0] : v[0];
+                    to[1] = kAdd ? to[1] + v[1] : v[1];
+                }
+            });
+        });
 }
 
 }  // namespace
@@ -132,16 +160,15 @@ cobalt_status launch_down_gradient(const Groups& g, const void* dout, Rows rows,
                                    void* dgate_up, hipStream_t s) {
     return by_act(act, [&](auto a) {
         return by_bool(d % 64 == 0, [&](auto whole) {
-            return by_shape(g, f, tiles(d, 64), [&](auto shape) {
+            return by_shape<Along::kRows>(g, f, [&](auto shape) {
                 typedef decltype(shape) S;
-                return over_tiles(most_tiles(g.M, g.E, S::kBM), tiles(f, S::kBN),
-                                  [&](uint32_t b0, unsigned n) {
-                                      down_gradient_kernel<S, a(), whole()>
-                                          <<<n, S::kThreads, 0, s>>>(
-                                              g, b0, (const char*)dout, rows, d, f,
-                                              (const char*)w_down, (const uint16_t*)gate_up,
-                                              (uint16_t*)dgate_up);
-                                  });
+                return over_tiles<S::kStays>(
+                    tile_grid(most_tiles(g.M, g.E, S::kBM), tiles(f, S::kBN)),
+                    [&](uint32_t b0, unsigned n, uint32_t all) {
+                        down_gradient_kernel<S, a(), whole()><<<n, S::kThreads, 0, s>>>(
+                            g, b0, all, (const char*)dout, rows, d, f, (const char*)w_down,
+                            (const uint16_t*)gate_up, (uint16_t*)dgate_up);
+                    });
             });
         });
     });
@@ -150,14 +177,15 @@ cobalt_status launch_down_gradient(const Groups& g, const void* dout, Rows rows,
 cobalt_status launch_gate_up_gradient(const Groups& g, const void* dgate_up, int64_t d, int64_t f,
                                       const void* w_in, Rows rows, void* dx, hipStream_t s) {
     return by_bool(f % 32 == 0, [&](auto whole) {
-        return by_shape(g, d, tiles(2 * f, 64), [&](auto shape) {
+        return by_shape<Along::kRows>(g, d, [&](auto shape) {
             typedef decltype(shape) S;
-            return over_tiles(most_tiles(g.M, g.E, S::kBM), tiles(d, S::kBN),
-                              [&](uint32_t b0, unsigned n) {
-                                  gate_up_gradient_kernel<S, whole()><<<n, S::kThreads, 0, s>>>(
-                                      g, b0, (const char*)dgate_up, d, f, (const char*)w_in, rows,
-                                      (uint16_t*)dx);
-                              });
+            return over_tiles<S::kStays>(
+                tile_grid(most_tiles(g.M, g.E, S::kBM), tiles(d, S::kBN)),
+                [&](uint32_t b0, unsigned n, uint32_t all) {
+                    gate_up_gradient_kernel<S, whole()><<<n, S::kThreads, 0, s>>>(
+                        g, b0, all, (const char*)dgate_up, d, f, (const char*)w_in, rows,
+                        (uint16_t*)dx);
+                });
         });
     });
 }
@@ -168,11 +196,12 @@ cobalt_status launch_weight_gradient(const Groups& g, const void* a, int64_t na,
     const auto run = [&](auto shape, auto in_float, auto in_add, auto ga, auto gb) {
         typedef decltype(shape) S;
         const int64_t mt = tiles(na, S::kBM);
-        return over_tiles(mt * g.E, tiles(nb, S::kBN), [&](uint32_t b0, unsigned n) {
-            weight_gradient_kernel<S, in_float(), in_add(), ga(), gb()>
-                <<<n, S::kThreads, 0, s>>>(g, b0, (uint32_t)mt, (const char*)a, na,
-                                           (const char*)b, nb, rows, dw);
-        });
+        return over_tiles<S::kStays>(
+            tile_grid(mt * g.E, tiles(nb, S::kBN)), [&](uint32_t b0, unsigned n, uint32_t all) {
+                weight_gradient_kernel<S, in_float(), in_add(), ga(), gb()>
+                    <<<n, S::kThreads, 0, s>>>(g, b0, all, (uint32_t)mt, (const char*)a, na,
+                                               (const char*)b, nb, rows, dw);
+            });
     };
     // rows without an index are the places; one operand at most has one
     const std::true_type yes;
@@ -186,7 +215,12 @@ cobalt_status launch_weight_gradient(const Groups& g, const void* a, int64_t na,
         if (!f32) return gather(shape, no, no);
         return add ? gather(shape, yes, yes) : gather(shape, yes, no);
     };
-    return by_type(Shape<4, 8>());
+    return by_shape<Along::kColumns>(
+        [&](auto shape) {
+            typedef decltype(shape) S;
+            return g.E * tiles(na, S::kBM) * tiles(nb, S::kBN);
+        },
+        by_type);
 }
 
 size_t expert_backward_workspace_bytes(int64_t, int, int64_t, int64_t) { return 256; }

@@ -45,7 +45,8 @@ __device__ __forceinline__ float act_slope(float g) {
 }
 
 // Tile `id` of the list of all experts' tiles of BM places: its expert and
-// places [lo, hi). False behind the last tile. Called by whole waves; every
+// places [lo, hi). 1; behind the last tile 0, or -1 if the list ends before
+// tile `first` (at most id) already. Called by whole waves; every
 // wave gets the same answer. Each lane counts the tiles of a run of experts,
 // the wave scans the counts, and the lane that holds the tile is found by a
 // ballot, so that no list has to be made by a launch of its own. Offsets
@@ -54,7 +55,8 @@ __device__ __forceinline__ float act_slope(float g) {
 struct Tile {
     int32_t e, lo, hi;
 };
-__device__ __forceinline__ bool find_tile(const Groups& g, int BM, uint32_t id, Tile* out) {
+__device__ __forceinline__ int find_tile(const Groups& g, int BM, uint32_t id, uint32_t first,
+                                         Tile* out) {
     const int lane = threadIdx.x & 63;
     const int per = (g.E + 63) / 64;
     const int e0 = min(lane * per, g.E), e1 = min(e0 + per, g.E);
@@ -76,7 +78,7 @@ __device__ __forceinline__ bool find_tile(const Groups& g, int BM, uint32_t id, 
         if (lane >= o) incl += up;
     }
     const uint64_t hit = __ballot(id - (incl - own) < own);
-    if (hit == 0) return false;
+    if (hit == 0) return first >= (uint32_t)__builtin_amdgcn_readlane((int)incl, 63) ? -1 : 0;
     const int src = __ffsll((unsigned long long)hit) - 1;
     uint32_t left =
         id - (uint32_t)__builtin_amdgcn_readlane((int)(incl - own), src);
@@ -93,7 +95,7 @@ __device__ __forceinline__ bool find_tile(const Groups& g, int BM, uint32_t id, 
     out->e = __builtin_amdgcn_readfirstlane(e);
     out->lo = __builtin_amdgcn_readfirstlane(lo + (int)left * BM);
     out->hi = min(__builtin_amdgcn_readfirstlane(hi), out->lo + BM);
-    return true;
+    return 1;
 }
 
 // Most tiles of BM places that M places of E experts can make.

@@ -128,7 +128,7 @@ __global__ __launch_bounds__(512) void gate_up_few_kernel(Groups g, uint32_t b0,
     __shared__ __attribute__((aligned(16))) float sums[kFewWaves * 2 * 256];
     const uint32_t nt = (uint32_t)((f + kCols - 1) / kCols), b = b0 + blockIdx.x;
     Tile t;
-    if (!find_tile(g, kFewPlaces, b / nt, &t)) return;
+    if (find_tile(g, kFewPlaces, b / nt, b / nt, &t) <= 0) return;
     const int64_t n0 = (int64_t)(b % nt) * kCols;
     const int i = threadIdx.x & 15, group = wave_id() / KS;
     const int64_t n = min(n0 + group * 16 + i, f - 1), first = (int64_t)t.e * 2 * f + n;
@@ -155,7 +155,7 @@ __global__ __launch_bounds__(512) void down_few_kernel(Groups g, uint32_t b0, Si
     __shared__ __attribute__((aligned(16))) float sums[kFewWaves * 256];
     const uint32_t nt = (uint32_t)((d + kCols - 1) / kCols), b = b0 + blockIdx.x;
     Tile t;
-    if (!find_tile(g, kFewPlaces, b / nt, &t)) return;
+    if (find_tile(g, kFewPlaces, b / nt, b / nt, &t) <= 0) return;
     const int64_t n0 = (int64_t)(b % nt) * kCols;
     const int i = threadIdx.x & 15, group = wave_id() / KS;
     const int64_t n = min(n0 + group * 16 + i, d - 1);
@@ -193,18 +193,20 @@ cobalt_status gate_up(const Groups& g, const Side& x, Rows rows, const Side& w, 
     return by_act(act, [&](auto a) {
         if (few_rows(g))
             return by_parts(w.bytes, [&](auto ks) {
-                return over_tiles(few_grid(g, f, ks()), [&](uint32_t b0, unsigned n) {
-                    gate_up_few_kernel<ks(), a(), Side><<<n, 512, 0, s>>>(
-                        g, b0, x, rows, w, f, (uint16_t*)h, (uint16_t*)gu);
-                });
+                return over_tiles<false>(
+                    few_grid(g, f, ks()), [&](uint32_t b0, unsigned n, uint32_t) {
+                        gate_up_few_kernel<ks(), a(), Side><<<n, 512, 0, s>>>(
+                            g, b0, x, rows, w, f, (uint16_t*)h, (uint16_t*)gu);
+                    });
             });
-        return by_shape(g, f * 2, tiles(w.bytes, kStepBytes), [&](auto shape) {
+        return by_shape<Side::kAlong>(g, f * 2, [&](auto shape) {
             typedef decltype(shape) S;
-            return over_tiles(most_tiles(g.M, g.E, S::kBM), tiles(f, S::kBN / 2),
-                              [&](uint32_t b0, unsigned n) {
-                                  gate_up_kernel<S, a(), Side><<<n, S::kThreads, 0, s>>>(
-                                      g, b0, x, rows, w, f, (uint16_t*)h, (uint16_t*)gu);
-                              });
+            return over_tiles<S::kStays>(
+                tile_grid(most_tiles(g.M, g.E, S::kBM), tiles(f, S::kBN / 2)),
+                [&](uint32_t b0, unsigned n, uint32_t all) {
+                    gate_up_kernel<S, a(), Side><<<n, S::kThreads, 0, s>>>(
+                        g, b0, all, x, rows, w, f, (uint16_t*)h, (uint16_t*)gu);
+                });
         });
     });
 }
@@ -214,18 +216,20 @@ cobalt_status down(const Groups& g, const Side& h, const Side& w, int64_t d, Row
                    hipStream_t s) {
     if (few_rows(g))
         return by_parts(w.bytes, [&](auto ks) {
-            return over_tiles(few_grid(g, d, ks()), [&](uint32_t b0, unsigned n) {
-                down_few_kernel<ks(), Side>
-                    <<<n, 512, 0, s>>>(g, b0, h, w, d, rows, (uint16_t*)out);
-            });
+            return over_tiles<false>(
+                few_grid(g, d, ks()), [&](uint32_t b0, unsigned n, uint32_t) {
+                    down_few_kernel<ks(), Side>
+                        <<<n, 512, 0, s>>>(g, b0, h, w, d, rows, (uint16_t*)out);
+                });
         });
-    return by_shape(g, d, tiles(w.bytes, kStepBytes), [&](auto shape) {
+    return by_shape<Side::kAlong>(g, d, [&](auto shape) {
         typedef decltype(shape) S;
-        return over_tiles(most_tiles(g.M, g.E, S::kBM), tiles(d, S::kBN),
-                          [&](uint32_t b0, unsigned n) {
-                              down_kernel<S, Side><<<n, S::kThreads, 0, s>>>(
-                                  g, b0, h, w, d, rows, (uint16_t*)out);
-                          });
+        return over_tiles<S::kStays>(
+            tile_grid(most_tiles(g.M, g.E, S::kBM), tiles(d, S::kBN)),
+            [&](uint32_t b0, unsigned n, uint32_t all) {
+                down_kernel<S, Side>
+                    <<<n, S::kThreads, 0, s>>>(g, b0, all, h, w, d, rows, (uint16_t*)out);
+            });
     });
 }
 

@@ -36,6 +36,9 @@ struct Shape {
     static constexpr int kWM = 2, kWN = WN, kTM = TM;
     static constexpr int kWaves = kWM * kWN, kThreads = 64 * kWaves;
     static constexpr int kBM = kWM * TM * 16, kBN = kWN * 64;
+    // two or three workgroups share a CU where the stages leave room for them;
+    // otherwise one stays there and goes from tile to tile
+    static constexpr bool kStays = 2 * (kBM + kBN) * 128 > 80 * 1024;
 };
 constexpr int kStepBytes = 128;
 
@@ -46,6 +49,14 @@ alignas(16) static __device__ const uint32_t kNothing[4] = {0, 0, 0, 0};
 __device__ __forceinline__ void load_to_lds(const char* p, char* lds) {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
                                      (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
+}
+
+// The thread's number, computed anew: what is made of it before and after the
+// steps of a tile shall not stay in registers during them.
+__device__ __forceinline__ int fresh_thread() {
+    int t = threadIdx.x;
+    asm volatile("" : "+v"(t));
+    return t;
 }
 
 __device__ __forceinline__ int wave_id() {
@@ -69,22 +80,23 @@ struct RowOperand {
     const char* base[kLoads];
     int64_t bytes;
 
-    __device__ __forceinline__ static int row_of(int j) {
-        return (j * kWaves + wave_id()) * 8 + (threadIdx.x & 63) / 8;
+    __device__ __forceinline__ static int row_of(int j, int thread) {
+        return (j * kWaves + wave_id()) * 8 + (thread & 63) / 8;
     }
     // the lane's chunk of the step, the same in all of its rows
-    __device__ __forceinline__ static int chunk() {
-        return (threadIdx.x & 7) ^ ((row_of(0) >> 1) & 7);
+    __device__ __forceinline__ static int chunk(int thread) {
+        return (thread & 7) ^ ((row_of(0, thread) >> 1) & 7);
     }
     // row(r): row r of the tile, as an address, or as an offset from first(r8)
     // with r8 = r / 8 * 8
     template <typename F, typename R>
     __device__ __forceinline__ void start(int64_t row_bytes, F&& first, R&& row) {
+        const int thread = fresh_thread();
         bytes = row_bytes;
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
             if constexpr (kNear) base[j] = first((j * kWaves + wave_id()) * 8);
-            p[j] = (At)row(row_of(j)) + chunk() * 16;
+            p[j] = (At)row(row_of(j, thread)) + chunk(thread) * 16;
         }
     }
     __device__ __forceinline__ const char* at(int j) const {
@@ -95,7 +107,7 @@ struct RowOperand {
     }
     __device__ __forceinline__ void load(char* lds, int s) {
         const int w = wave_id();
-        if (kWhole || chunk() * 16 < bytes - (int64_t)s * kStepBytes) {
+        if (kWhole || chunk(threadIdx.x) * 16 < bytes - (int64_t)s * kStepBytes) {
 #pragma unroll
             for (int j = 0; j < kLoads; ++j) load_to_lds(at(j), lds + (j * kWaves + w) * 1024);
         } else {  // behind the end of the rows: zeros, on both sides of a product
@@ -134,12 +146,16 @@ struct ColumnOperand {
     static constexpr int kRowBytes = 2 * B;
     static constexpr int kWaves = S::kWaves, kLoads = B * 128 / 1024 / kWaves;
     static constexpr int kReads = 2;
+    static_assert(1024 % kRowBytes == 0, "a wave's load is whole rows");
     const char* base;  // first column of the tile, in row 0 or in the step's first row
     int64_t pitch;     // bytes between rows
     int rows;          // k
     const int32_t* idx;
     uint32_t n_rows;
-    uint32_t at[kLoads];    // byte of the lane's chunk in the row (kGather) or the step
+    // A lane's loads are kApart rows apart, and its chunk of them is the same,
+    // or the same of every second one.
+    static constexpr int kApart = kWaves * (1024 / kRowBytes), kAts = kApart == 16 ? 2 : 1;
+    uint32_t at[kAts];      // byte of the chunk in the row; from the first load's row (!kGather)
     uint32_t next[kLoads];  // rows of the step to come (kGather)
 
     // bit0, bit1: bits 0 and 1 of k; bit4: its bit 4
@@ -147,24 +163,25 @@ struct ColumnOperand {
         // rows of 128 bytes: even and odd ones lie in different banks already
         return B == 64 ? bit1 | bit4 << 1 : bit0 | bit1 << 1 | bit4 << 2;
     }
-    __device__ __forceinline__ static int row_of(int j) {
-        return (j * kWaves + wave_id()) * (1024 / kRowBytes) + (threadIdx.x & 63) * 16 / kRowBytes;
+    __device__ __forceinline__ static int row_of(int j, int thread) {
+        return j * kApart + wave_id() * (1024 / kRowBytes) + (thread & 63) * 16 / kRowBytes;
     }
     // cols: columns from `first` on that there are (a multiple of 8)
     __device__ __forceinline__ void start(const void* first, int64_t cols, int64_t row_bytes,
                                           int k, const int32_t* index, int64_t index_rows) {
-        const int lane = threadIdx.x & 63;
+        const int thread = fresh_thread(), lane = thread & 63;
         base = (const char*)first;
         pitch = row_bytes;
         rows = k;
         idx = index;
         n_rows = (uint32_t)min(index_rows, int64_t(1) << 31);
 #pragma unroll
-        for (int j = 0; j < kLoads; ++j) {
-            const int r = row_of(j), slot = lane * 16 % kRowBytes / 16;
+        for (int j = 0; j < kAts; ++j) {
+            const int r = row_of(j, thread), slot = lane * 16 % kRowBytes / 16;
             const int unit = (slot >> 1) ^ place(r & 1, (r >> 1) & 1, (r >> 4) & 1);
             const int c = (unit * 2 + (slot & 1)) * 8;
-            at[j] = (c < cols ? c : (int)cols - 8) * 2 + (kGather ? 0 : r * (uint32_t)pitch);
+            at[j] = (c < cols ? c : (int)cols - 8) * 2 +
+                    (kGather ? 0 : row_of(0, thread) * (uint32_t)pitch);
         }
         if (kGather) fetch(0);
     }
@@ -172,7 +189,7 @@ struct ColumnOperand {
     __device__ __forceinline__ void fetch(int s) {
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
-            const int k = s * 64 + row_of(j);
+            const int k = s * 64 + row_of(j, threadIdx.x);
             const int r = idx[min(k, rows - 1)];
             next[j] = k < rows ? (uint32_t)r : ~0u;
         }
@@ -183,11 +200,12 @@ struct ColumnOperand {
         for (int j = 0; j < kLoads; ++j) {
             char* to = lds + (j * kWaves + w) * 1024;
             if constexpr (kGather) {
-                const char* p = base + at[j] + (uint64_t)next[j] * (uint32_t)pitch;
+                const char* p = base + at[j % kAts] + (uint64_t)next[j] * (uint32_t)pitch;
                 load_to_lds(next[j] < n_rows ? p : (const char*)kNothing, to);
             } else {
-                const char* p = base + at[j];
-                load_to_lds(kWhole || s * 64 + row_of(j) < rows ? p : (const char*)kNothing, to);
+                const char* p = base + j * kApart * pitch + at[j % kAts];
+                const bool ok = kWhole || s * 64 + row_of(j, threadIdx.x) < rows;
+                load_to_lds(ok ? p : (const char*)kNothing, to);
             }
         }
         if constexpr (kGather)
@@ -215,7 +233,9 @@ using Acc = f32x4[TM][4];
 template <typename S>
 struct Bf16Math {
     static constexpr int kLds = 0, kReads = 0;
-    __device__ __forceinline__ void prefetch(int) {}
+    __device__ __forceinline__ void issue(int) {}
+    __device__ __forceinline__ void begin(char*, int) {}
+    __device__ __forceinline__ void prefetch() {}
     __device__ __forceinline__ void commit(char*, int) {}
     __device__ __forceinline__ void read(const char*, int) {}
     __device__ __forceinline__ void advance() {}
@@ -243,7 +263,8 @@ __device__ __forceinline__ f32x4 mx_product(const bf16x8& p, const bf16x8& q, co
 // one scale byte of its row for each half of a step, and the two are
 // neighbours. The eight scale bytes of a row and step come through registers
 // (rows of scales need not be aligned) into LDS, one dword per thread and
-// operand. There the two bytes of row r and chunk pair g lie next to those of
+// operand, loaded a step before they are written there and written a step
+// before they are read. There the two bytes of row r and chunk pair g lie next to those of
 // row r + 16 (r % 32 < 16), so that one dword serves a lane for two tiles.
 template <typename S, bool kWhole>
 struct MxMath {
@@ -254,14 +275,15 @@ struct MxMath {
     const char* base;  // of the row of p: at a 32-bit offset from here
     uint32_t p;
     int left;          // bytes from there to the rows' end
-    uint32_t next_q, next_p;
+    uint32_t next_q, next_p;        // dwords of the step that is written next
+    uint32_t first_q[2], first_p[2];  // of the first two steps
     uint32_t sq[2][TM / 2], sp[2][2];  // of this step, of the next
 
     // row_q(r): scales of row r of q; row_p(r): of p, as an offset from `first`,
     // the same for a wave; n: scales of a row
     template <typename FQ, typename FP>
     __device__ __forceinline__ void start(int64_t n, FQ&& row_q, const char* first, FP&& row_p) {
-        const int r = threadIdx.x / 2, at = threadIdx.x % 2 * 4;
+        const int thread = fresh_thread(), r = thread / 2, at = thread % 2 * 4;
         q = (const char*)row_q(r < kBM ? r : kBM - 1) + at;
         base = first;
         p = (uint32_t)row_p(r) + at;
@@ -278,12 +300,23 @@ struct MxMath {
         }
         return v;
     }
-    __device__ __forceinline__ void prefetch(int) {
-        if (kBM == kBN || threadIdx.x < kBM * 2) next_q = dword(q, left);
-        next_p = dword(base + p, left);
+    __device__ __forceinline__ void fetch(uint32_t* to_q, uint32_t* to_p) {
+        if (kBM == kBN || threadIdx.x < kBM * 2) *to_q = dword(q, left);
+        *to_p = dword(base + p, left);
         q += 8;
         base += 8;
         left -= 8;
+    }
+    __device__ __forceinline__ void prefetch() { fetch(&next_q, &next_p); }
+    // the loads of the first three steps, and the writes of two
+    __device__ __forceinline__ void issue(int steps) {
+        fetch(&first_q[0], &first_p[0]);
+        if (steps > 1) fetch(&first_q[1], &first_p[1]);
+        if (steps > 2) prefetch();
+    }
+    __device__ __forceinline__ void begin(char* lds, int steps) {
+        write(lds, 0, first_q[0], first_p[0]);
+        if (steps > 1) write(lds, 1, first_q[1], first_p[1]);
     }
     __device__ __forceinline__ static void put(char* lds, uint32_t v) {
         const int r = threadIdx.x / 2, g = threadIdx.x % 2 * 2;
@@ -291,11 +324,12 @@ struct MxMath {
         to[0] = (uint16_t)v;
         to[2] = (uint16_t)(v >> 16);
     }
-    __device__ __forceinline__ void commit(char* lds, int s) {
+    __device__ __forceinline__ static void write(char* lds, int s, uint32_t vq, uint32_t vp) {
         char* to = lds + (s & 1) * (kLds / 2);
-        if (kBM == kBN || threadIdx.x < kBM * 2) put(to, next_q);
-        put(to + kBM * 8, next_p);
+        if (kBM == kBN || threadIdx.x < kBM * 2) put(to, vq);
+        put(to + kBM * 8, vp);
     }
+    __device__ __forceinline__ void commit(char* lds, int s) { write(lds, s, next_q, next_p); }
     // the scales of step s, for both halves
     __device__ __forceinline__ void read(const char* lds, int s) {
         const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4, w = wave_id();
@@ -334,102 +368,171 @@ struct MxMath {
     }
 };
 
-// LDS of a tile: two stages, and what the products need besides.
-template <typename S, typename Math>
-constexpr size_t tile_lds() {
-    return 2 * (size_t)(S::kBM + S::kBN) * kStepBytes + Math::kLds;
-}
+// Floats of LDS in which a wave turns its results (store_rows).
+constexpr int kTurn = 16 * 64;
 
+// LDS of a tile: two stages, what the products need besides, and room to turn
+// the results, which may be the stages' if no further tile is loaded there.
+template <typename S, typename Math, bool kTurns>
+struct Lds {
+    static constexpr int kStage = (S::kBM + S::kBN) * kStepBytes;
+    static constexpr int kTurnBytes = S::kWaves * kTurn * 4;
+    static constexpr int kTiles = 2 * kStage + Math::kLds;
+    static constexpr int kBytes = kTiles + (kTurns && S::kStays ? kTurnBytes : 0);
+    static_assert(kTurnBytes <= 2 * kStage && kBytes <= 160 * 1024, "LDS of a CU");
+    __device__ static char* turn(char* lds) { return lds + (S::kStays ? kTiles : 0); }
+};
+
+// The steps of a tile. issue() begins the loads of the first two into LDS,
+// which no wave reads at that time; after arrive() the wave's part of them is
+// there, and run() does the rest. Results of the tile before are stored between
+// the two: then run() does not wait for those stores until its second step.
 template <typename S, typename Q, typename P, typename Math>
-__device__ __forceinline__ void multiply(char* lds, Q& q, P& p, Math& math, int steps,
-                                         Acc<S::kTM>& acc) {
-    constexpr int TM = S::kTM, kBM = S::kBM, kStage = (kBM + S::kBN) * kStepBytes;
-    const int w = wave_id(), m0 = w / S::kWN * (TM * 16), n0 = w % S::kWN * 64;
-    char* extra = lds + 2 * kStage;
-    bf16x8 fq[2][TM], fp[2][4];
-    const auto load = [&](int s) {
+struct Pipe {
+    static constexpr int TM = S::kTM, kBM = S::kBM, kStage = (kBM + S::kBN) * kStepBytes;
+    char* lds;
+    Q q;
+    P p;
+    Math math;
+
+    __device__ __forceinline__ void load(int s) {
         char* at = lds + (s & 1) * kStage;
-        math.prefetch(s);
         q.load(at, s);
         p.load(at + kBM * kStepBytes, s);
-    };
-    const auto read = [&](int to, int s, int kk) {
-        const char* at = lds + (s & 1) * kStage;
-        if (kk == 0) math.read(extra, s);
-#pragma unroll
-        for (int t = 0; t < 4; ++t) fp[to][t] = P::read(at + kBM * kStepBytes, n0, t, kk);
-#pragma unroll
-        for (int t = 0; t < TM; ++t) fq[to][t] = Q::read(at, m0, t, kk);
-    };
-    // the products of half kk, and the reads of the half after it
-    const auto half = [&](int kk, int s) {
-        read(kk ^ 1, s + kk, kk ^ 1);
-#pragma unroll
-        for (int x = 0; x < TM; ++x)
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-                acc[x][t] = math.product(fp[kk][t], fq[kk][x], acc[x][t], x, t, kk);
-        constexpr int kR = TM * Q::kReads + 4 * P::kReads + Math::kReads, kM = 4 * TM;
-        constexpr int kPer = kM / kR > 0 ? kM / kR : 1;
-        constexpr int kGroups = kM / kPer < kR ? kM / kPer : kR;
-#pragma unroll
-        for (int i = 0; i < kGroups; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);    // a read of LDS
-            __builtin_amdgcn_sched_group_barrier(0x008, kPer, 0);  // kPer products
-        }
-        // holds the products here: nothing else would keep the compiler from
-        // moving them past the barrier, behind the wait that they should fill
-#pragma unroll
-        for (int x = 0; x < TM; ++x)
-#pragma unroll
-            for (int t = 0; t < 4; ++t) asm volatile("" : "+v"(acc[x][t]));
-        __builtin_amdgcn_sched_barrier(0);
-    };
-#pragma unroll
-    for (int x = 0; x < TM; ++x)
-#pragma unroll
-        for (int t = 0; t < 4; ++t) acc[x][t] = f32x4{0, 0, 0, 0};
-    load(0);
-    math.commit(extra, 0);
-    if (steps > 1) load(1);
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    read(0, 0, 0);
-    math.advance();
-    for (int s = 0; s < steps; ++s) {
-        half(0, s);
-        // every wave has read stage s and has its part of stage s + 1
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        math.commit(extra, s + 1);
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (s + 2 < steps) load(s + 2);
-        __builtin_amdgcn_sched_barrier(0);
-        half(1, s);  // behind the last step: reads that nothing uses
-        math.advance();
     }
-    // no wave still reads LDS when the tile's results go through it
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    __device__ __forceinline__ void issue(int steps) {
+        if (steps == 0) return;
+        load(0);
+        if (steps > 1) load(1);
+        math.issue(steps);
+    }
+    __device__ __forceinline__ void arrive() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+    __device__ __forceinline__ void run(int steps, Acc<TM>& acc) {
+        const int w = wave_id(), m0 = w / S::kWN * (TM * 16), n0 = w % S::kWN * 64;
+        char* extra = lds + 2 * kStage;
+        bf16x8 fq[2][TM], fp[2][4];
+        const auto read = [&](int to, int s, int kk) {
+            const char* at = lds + (s & 1) * kStage;
+            if (kk == 0) math.read(extra, s);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) fp[to][t] = P::read(at + kBM * kStepBytes, n0, t, kk);
+#pragma unroll
+            for (int t = 0; t < TM; ++t) fq[to][t] = Q::read(at, m0, t, kk);
+        };
+        // the products of half kk, and the reads of the half after it
+        const auto half = [&](int kk, int s) {
+            read(kk ^ 1, s + kk, kk ^ 1);
+#pragma unroll
+            for (int x = 0; x < TM; ++x)
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+                    acc[x][t] = math.product(fp[kk][t], fq[kk][x], acc[x][t], x, t, kk);
+            constexpr int kR = TM * Q::kReads + 4 * P::kReads + Math::kReads, kM = 4 * TM;
+            constexpr int kPer = kM / kR > 0 ? kM / kR : 1;
+            constexpr int kGroups = kM / kPer < kR ? kM / kPer : kR;
+#pragma unroll
+            for (int i = 0; i < kGroups; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);     // a read of LDS
+                __builtin_amdgcn_sched_group_barrier(0x008, kPer, 0);  // kPer products
+            }
+            // holds the products here: nothing else would keep the compiler from
+            // moving them past the barrier, behind the wait that they should fill
+#pragma unroll
+            for (int x = 0; x < TM; ++x)
+#pragma unroll
+                for (int t = 0; t < 4; ++t) asm volatile("" : "+v"(acc[x][t]));
+            __builtin_amdgcn_sched_barrier(0);
+        };
+#pragma unroll
+        for (int x = 0; x < TM; ++x)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) acc[x][t] = f32x4{0, 0, 0, 0};
+        if (steps == 0) return;
+        math.begin(extra, steps);
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        read(0, 0, 0);
+        math.advance();
+        for (int s = 0; s < steps; ++s) {
+            half(0, s);
+            // every wave has read stage s and has its part of stage s + 1
+            if (s > 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            if (s + 2 < steps) {
+                math.commit(extra, s + 2);
+                load(s + 2);
+                if (s + 3 < steps) math.prefetch();
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            half(1, s);  // behind the last step: reads that nothing uses
+            math.advance();
+        }
+        // no wave still reads the stages when this one goes on
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    }
+};
+
+// Makes the tiles b, b + gridDim.x, ... below `all` (shapes that stay on their
+// CU) or tile b. find(b, &job): whether there is such a tile, 0 if not, -1 if
+// there is none from there on; start(job): its operands; job.steps: its steps;
+// finish(job, acc): stores the results. The next tile is found while the first
+// loads of a tile are under way, and its own first loads are begun before the
+// results are stored: without that a tile of six steps takes as long to begin
+// and to end as to multiply.
+template <typename S, typename Job, typename Pi, typename Fi, typename St, typename Fn>
+__device__ __forceinline__ void make_tiles(Pi& pipe, uint32_t b, uint32_t all, Fi&& find,
+                                           St&& start, Fn&& finish) {
+    const auto from = [&](Job* job) {
+        for (; b < all; b += gridDim.x) {
+            const int found = find(b, job);
+            if (found > 0) return true;
+            if (found < 0 || !S::kStays) return false;
+        }
+        return false;
+    };
+    Job job;
+    if (!from(&job)) return;
+    start(job);
+    pipe.issue(job.steps);
+    pipe.arrive();
+    for (;;) {
+        Job next;
+        bool more = false;
+        if constexpr (S::kStays) {
+            b += gridDim.x;
+            more = from(&next);
+        }
+        Acc<S::kTM> acc;
+        pipe.run(job.steps, acc);
+        if (more) {
+            start(next);
+            pipe.issue(next.steps);
+            pipe.arrive();
+        }
+        finish(job, acc);
+        if (!more) return;
+        job = next;
+    }
 }
 
-// Calls store(m, n, v) for the results of a tile after multiply(), eight
-// consecutive n (n % 8 == 0) per lane and whole 128-byte lines of n per
-// instruction: each wave turns its results in LDS, 16 rows of m at a time.
+// Calls store(m, n, v) for the results of a tile, eight consecutive n
+// (n % 8 == 0) per lane and whole 128-byte lines of n per instruction: each
+// wave turns its results in its part of `turn`, 16 rows of m at a time. Four
+// floats u of row m lie at u ^ m, so that the 16 rows that a quarter wave
+// writes at one u lie in 16 different groups of banks.
 template <typename S, typename F>
-__device__ __forceinline__ void store_rows(char* lds, const Acc<S::kTM>& acc, F&& store) {
-    constexpr int kPitch = 64 + 4;  // floats: rows shifted by four banks
-    const int lane = threadIdx.x & 63, w = wave_id();
-    float* part = (float*)lds + w * 16 * kPitch;
+__device__ __forceinline__ void store_rows(char* turn, const Acc<S::kTM>& acc, F&& store) {
+    const int lane = fresh_thread() & 63, w = wave_id(), i = lane & 15;
+    f32x4* part = (f32x4*)turn + w * (kTurn / 4);
     const int m0 = w / S::kWN * (S::kTM * 16), n0 = w % S::kWN * 64;
 #pragma unroll
     for (int y = 0; y < S::kTM; ++y) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            *(f32x4*)(part + (lane & 15) * kPitch + k * 16 + (lane >> 4) * 4) = acc[y][k];
+        for (int k = 0; k < 4; ++k) part[i * 16 + ((k * 4 + (lane >> 4)) ^ i)] = acc[y][k];
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            const int m = half * 8 + lane / 8, n = lane % 8 * 8;
-            const f32x4 v[2] = {*(const f32x4*)(part + m * kPitch + n),
-                                *(const f32x4*)(part + m * kPitch + n + 4)};
-            store(m0 + y * 16 + m, n0 + n, v);
+            const int m = half * 8 + lane / 8, u = lane % 8 * 2;
+            const f32x4 v[2] = {part[m * 16 + (u ^ m)], part[m * 16 + ((u + 1) ^ m)]};
+            store(m0 + y * 16 + m, n0 + u * 4, v);
         }
     }
 }
@@ -441,14 +544,15 @@ __device__ __forceinline__ void store_rows(char* lds, const Acc<S::kTM>& acc, F&
 struct TileAt {
     uint32_t m, n;
 };
+constexpr uint32_t kBand = 4;
 __device__ __forceinline__ TileAt tile_at(uint32_t b, uint32_t nt) {
     const uint32_t id = b / 256 * 256 + b % 8 * 32 + b / 8 % 32;
-    const uint32_t band = id / (4 * nt), r = id % (4 * nt);
-    return {band * 4 + r % 4, r / 4};
+    const uint32_t band = id / (kBand * nt), r = id % (kBand * nt);
+    return {band * kBand + r % kBand, r / kBand};
 }
 // Workgroups of a launch over mt x nt tiles.
 inline int64_t tile_grid(int64_t mt, int64_t nt) {
-    return ((mt + 3) / 4 * 4 * nt + 255) / 256 * 256;
+    return ((mt + kBand - 1) / kBand * kBand * nt + 255) / 256 * 256;
 }
 
 __device__ __forceinline__ float low(uint32_t v) { return __uint_as_float(v << 16); }
@@ -467,6 +571,22 @@ __device__ __forceinline__ u32x2 pack4(const f32x4& a) {
 
 // Places [lo, hi) of a tile as rows of x for the operand q: a place without a
 // row reads `other`, any row of the same length, and its results are not used.
+// A tile of rows as a job of make_tiles().
+struct RowJob {
+    Tile t;
+    int64_t n0;  // its first column
+    int steps;
+};
+// Job b among the tiles of kBM places by nt tiles of `cols` columns.
+template <typename S>
+__device__ __forceinline__ int find_rows(const Groups& g, uint32_t b, uint32_t nt, int cols,
+                                         RowJob* job) {
+    const TileAt at = tile_at(b, nt);
+    const int found = find_tile(g, S::kBM, at.m, at.m / kBand * kBand, &job->t);
+    job->n0 = (int64_t)at.n * cols;
+    return found;
+}
+
 template <typename S, int B, bool kWhole>
 __device__ __forceinline__ void start_rows(RowOperand<S, B, false, kWhole>& q, const Tile& t, const char* x,
                                            const Rows& rows, const char* other, int64_t bytes) {
@@ -476,31 +596,92 @@ __device__ __forceinline__ void start_rows(RowOperand<S, B, false, kWhole>& q, c
     });
 }
 
-// Launches kernel(b0, n) over ranges [b0, b0 + n) of `all` workgroups of at
-// most 512 threads that a grid can hold.
-template <typename F>
+// Launches kernel(b0, n, all) for `all` workgroups of at most 512 threads: over
+// ranges [b0, b0 + n) that a grid can hold, or once for workgroups that stay.
+template <bool kStays, typename F>
 cobalt_status over_tiles(int64_t all, F&& kernel) {
-    const int64_t most = kMaxLaunchItems / 512 / 256 * 256;
-    if (all > UINT32_MAX) return COBALT_EUNSUPPORTED;
+    constexpr int64_t kCus = 256;
+    const int64_t most = kStays ? kCus : kMaxLaunchItems / 512 / 256 * 256;
+    if (all > INT32_MAX) return COBALT_EUNSUPPORTED;
     for (int64_t b0 = 0; b0 < all; b0 += most) {
-        kernel((uint32_t)b0, (unsigned)std::min(all - b0, most));
+        kernel((uint32_t)b0, (unsigned)std::min(all - b0, most), (uint32_t)all);
         COBALT_LAUNCH_CHECK();
+        if (kStays) break;
     }
     return COBALT_OK;
 }
-template <typename F>
-cobalt_status over_tiles(int64_t mt, int64_t nt, F&& kernel) {
-    return over_tiles(tile_grid(mt, nt), kernel);
+
+// The tiles of a product are chosen by what they are expected to take: rounds
+// of workgroups over the 256 CUs, times what the workgroups that share a CU
+// work at once, in units of 32 x 256 results. Tiles that fill LDS less let
+// two or three workgroups share a CU, but read more of it per product. With
+// 16384 rows of 8 experts, 7168 x 2048, a unit and step takes (gate_up)
+//   bf16:  256 x 256 0.237 us, 192 x 256 0.238, 64 x 256 0.29, 64 x 128 0.39
+//   4-bit: 192 x 256 0.33 us, 128 x 256 0.38, 64 x 128 0.56 (256 x 256 does
+//          not fit into the registers with the scales: 0.47)
+// Tile by tile, with 256 x 256 | 192 x 256 | 64 x 256 | 64 x 128, in us:
+//   gate_up   16384 rows,   8 experts, 7168 x 2048:  1062 |  963 | 1184 | 1456
+//   its dh    16384 rows,   8 experts, 7168 x 2048:   760 |  644 |  737 |  906
+//   its dh    24576 rows,  64 experts, 2048 x 1024:   208 |  256 |  223 |  260
+//   gate_up    4096 rows, 128 experts, 2048 x 1024:   319 |  299 |  242 |  256
+//   gate_up    1018 rows,  16 experts,  512 x  256:    23 |   19 |   12 |   10
+struct Choice {
+    int64_t tiles;
+    int per_cu;   // workgroups that fit on a CU
+    double work;  // of a tile
+    double cost() const {
+        constexpr int64_t kCus = 256;
+        const int64_t side = std::max<int64_t>(1, std::min<int64_t>(per_cu, tiles / kCus + 1));
+        return (double)((tiles + kCus * side - 1) / (kCus * side)) * side * work;
+    }
+};
+// Tiles that M places of E experts are expected to make: half a tile more
+// than full ones for each expert.
+inline int64_t expected_tiles(const Groups& g, int BM) {
+    return g.M / BM + (std::min<int64_t>(g.E, g.M) + 1) / 2;
 }
 
-// Calls f(shape) with the tiles for M places of E experts, n columns and
-// `steps` steps of k.
-template <typename F>
-cobalt_status by_shape(const Groups& g, int64_t n, int64_t steps, F&& f) {
-    const int64_t mean = g.M / g.E;
-    if (mean <= 64) return f(Shape<4, 2>());
-    if (mean <= 128) return f(Shape<4, 4>());
-    return f(Shape<4, 8>());
+// What the rows of a product's tiles are: rows in memory, of bf16 or 4-bit
+// values, or columns.
+enum class Along { kRows, kMxRows, kColumns };
+
+// Calls f(shape) with the shape whose count(shape) tiles cost least.
+template <Along kAlong, typename C, typename F>
+cobalt_status by_shape(C&& count, F&& f) {
+    const Shape<2, 2> small;
+    const Choice few{count(small), 3, 1.95};
+    if constexpr (kAlong == Along::kMxRows) {
+        const Shape<4, 4> middle;
+        const Shape<4, 6> large;
+        const double a = few.cost(), b = Choice{count(middle), 1, 4.6}.cost(),
+                     c = Choice{count(large), 1, 6.0}.cost();
+        return c <= a && c <= b ? f(large) : b <= a ? f(middle) : f(small);
+    } else {
+        const Shape<4, 2> low;
+        const Shape<4, 8> large;
+        const double a = few.cost(), b = Choice{count(low), 2, 2.8}.cost(),
+                     c = Choice{count(large), 1, 8.0}.cost();
+        const auto others = [&] {
+            return c <= a && c <= b ? f(large) : b <= a ? f(low) : f(small);
+        };
+        if constexpr (kAlong == Along::kColumns) {
+            return others();
+        } else {
+            const Shape<2, 6> high;
+            const double d = Choice{count(high), 2, 3.25}.cost();
+            return d < a && d < b && d < c ? f(high) : others();
+        }
+    }
+}
+// The same for n columns of the experts' places.
+template <Along kAlong, typename F>
+cobalt_status by_shape(const Groups& g, int64_t n, F&& f) {
+    return by_shape<kAlong>(
+        [&](auto shape) {
+            typedef decltype(shape) S;
+            return expected_tiles(g, S::kBM) * ((n + S::kBN - 1) / S::kBN);
+        },
+        f);
 }
 
 // Calls f(act) with the activation as a constant.
