@@ -76,8 +76,10 @@ __device__ __forceinline__ void stream_products(float* sums, const Side& x, int6
             const int c = min((s + a) * 4 + g, chunks - 1);
 #pragma unroll
             for (int k = 0; k < S; ++k) p[to][a][k].load(w, row[k], c);
-            q[to][a].load(from, q_row, c);
         }
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a)
+            q[to][a].load(from, q_row, min((s + a) * 4 + g, chunks - 1));
         __builtin_amdgcn_sched_barrier(0);
     };
     const auto multiply = [&](int of, int s) {
@@ -199,7 +201,7 @@ cobalt_status gate_up(const Groups& g, const Side& x, Rows rows, const Side& w, 
                             g, b0, x, rows, w, f, (uint16_t*)h, (uint16_t*)gu);
                     });
             });
-        return by_shape<Side::kAlong>(g, f * 2, [&](auto shape) {
+        return by_shape<Side::kAlong>(g, f * 2, tiles(w.bytes, kStepBytes), [&](auto shape) {
             typedef decltype(shape) S;
             return over_tiles<S::kStays>(
                 tile_grid(most_tiles(g.M, g.E, S::kBM), tiles(f, S::kBN / 2)),
@@ -222,7 +224,7 @@ cobalt_status down(const Groups& g, const Side& h, const Side& w, int64_t d, Row
                         <<<n, 512, 0, s>>>(g, b0, h, w, d, rows, (uint16_t*)out);
                 });
         });
-    return by_shape<Side::kAlong>(g, d, [&](auto shape) {
+    return by_shape<Side::kAlong>(g, d, tiles(w.bytes, kStepBytes), [&](auto shape) {
         typedef decltype(shape) S;
         return over_tiles<S::kStays>(
             tile_grid(most_tiles(g.M, g.E, S::kBM), tiles(d, S::kBN)),

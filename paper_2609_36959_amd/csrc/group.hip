@@ -1,19 +1,20 @@
 // Pairs grouped by expert: a stable counting sort of the T*K pairs by their
 // expert, in the order in which the experts' products take their rows.
 //
-// place_kernel: a workgroup takes a tile of consecutive pairs, each wave a
-// segment of it. The waves count their pairs by expert in histograms of their
-// own in LDS; the first place of each (wave, expert) follows from the totals
-// of all tiles, the counts of the tiles before and those of the waves before.
-// Then each wave goes through its segment again, 64 pairs at a time: lanes of
-// the same expert find each other by one ballot per bit of the expert, so a
-// pair's place is the wave's next place of its expert plus the number of its
-// peers in lower lanes. No order depends on scheduling.
+// place_kernel: a workgroup takes a tile of consecutive pairs, up to 8192 at a
+// time; each wave takes a part of them, eight pairs per lane in registers. The
+// waves count their pairs by expert in histograms of their own in LDS; the
+// first place of each (wave, expert) follows from the totals of all tiles, the
+// counts of the tiles before and those of the waves before. Then each wave
+// goes through its pairs again, 64 at a time: lanes of the same expert find
+// each other by one ballot per bit of the expert, so a pair's place is the
+// wave's next place of its expert plus the number of its peers in lower lanes.
+// No order depends on scheduling.
 //
-// With one tile (up to kOneTile pairs) that is the whole call, one launch.
-// Above, count_kernel first writes the counts of every tile, [tiles][E], and
-// each workgroup of place_kernel sums them for itself (they come out of the
-// L2): that costs less than a third launch.
+// With one tile that is the whole call, one launch. Above, count_kernel first
+// writes the counts of every tile, [tiles][E], and each workgroup of
+// place_kernel sums them for itself (they come out of the L2): that costs less
+// than a third launch.
 #include <algorithm>
 
 #include "internal.hpp"
@@ -21,8 +22,8 @@
 namespace cobalt {
 namespace {
 
-// Pairs that one workgroup sorts by itself, and the most tiles beyond.
-constexpr int64_t kOneTile = 8192;
+constexpr int kChunks = 8;             // pairs of a lane
+constexpr int kTilePairs = 16 * 64 * kChunks;
 constexpr int64_t kMaxTiles = 256;
 
 struct Cut {
@@ -33,11 +34,12 @@ struct Cut {
 
 Cut cut_pairs(int64_t P, int E) {
     Cut c;
-    // 1024 to a wave keeps the walk short; at most kMaxTiles
-    c.tiles = (int)std::min<int64_t>(P <= kOneTile ? 1 : (P + kOneTile - 1) / kOneTile, kMaxTiles);
-    c.tile = std::max<int64_t>((P + c.tiles - 1) / c.tiles, 1);
+    // tiles of a workgroup's registers, or as much longer as keeps them few
+    const int64_t most = (P + kMaxTiles - 1) / kMaxTiles;
+    c.tile = std::max<int64_t>((most + kTilePairs - 1) / kTilePairs * kTilePairs, kTilePairs);
+    c.tiles = (int)std::max<int64_t>((P + c.tile - 1) / c.tile, 1);
     // as many waves as have pairs, and whose histograms leave room in LDS
-    const int64_t want = std::min<int64_t>((c.tile + 63) / 64, 16);
+    const int64_t want = std::min<int64_t>((P + 63) / 64, 16);
     const int64_t room = 64 * 1024 / (4 * (int64_t)E) - 2;
     c.waves = (int)std::max<int64_t>(1, std::min(want, room));
     c.lds = (size_t)(c.waves + 2) * E * 4;
@@ -48,17 +50,24 @@ __global__ __launch_bounds__(1024) void count_kernel(const int32_t* __restrict__
                                                      int E, int64_t tile,
                                                      uint32_t* __restrict__ counts) {
     extern __shared__ uint32_t hist[];
-    for (int e = threadIdx.x; e < E; e += blockDim.x) hist[e] = 0;
+    for (int e = threadIdx.x; e < E; e += 1024) hist[e] = 0;
     __syncthreads();
     const int64_t p0 = blockIdx.x * tile, p1 = p0 + tile < P ? p0 + tile : P;
-    for (int64_t p = p0 + threadIdx.x; p < p1; p += blockDim.x) {
-        const uint32_t e = (uint32_t)topk[p];
-        if (e < (uint32_t)E) atomicAdd(hist + e, 1u);
+    for (int64_t b = p0 + threadIdx.x; b < p1; b += 1024 * kChunks) {
+        uint32_t e[kChunks];
+#pragma unroll
+        for (int k = 0; k < kChunks; ++k)
+            e[k] = b + k * 1024 < p1 ? (uint32_t)topk[b + k * 1024] : ~0u;
+#pragma unroll
+        for (int k = 0; k < kChunks; ++k)
+            if (e[k] < (uint32_t)E) atomicAdd(hist + e[k], 1u);
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < E; e += blockDim.x) counts[(int64_t)blockIdx.x * E + e] = hist[e];
+    for (int e = threadIdx.x; e < E; e += 1024) counts[(int64_t)blockIdx.x * E + e] = hist[e];
 }
 
+// kOne: one tile, whose totals it counts itself.
+template <bool kOne>
 __global__ __launch_bounds__(1024) void place_kernel(
     const int32_t* __restrict__ topk, const int32_t* __restrict__ pos, int64_t P, int K, int E,
     int ebits, int64_t tile, int tiles, const uint32_t* __restrict__ counts,
@@ -66,87 +75,120 @@ __global__ __launch_bounds__(1024) void place_kernel(
     extern __shared__ uint32_t lds[];
     __shared__ uint32_t wave_sum[16];
     const int waves = blockDim.x >> 6, w = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    uint32_t* total = lds;            // [E]: pairs of the expert, then its first place
-    uint32_t* before = lds + E;       // [E]: of them, in the tiles before
-    uint32_t* hist = lds + 2 * E;     // [waves][E]: of the wave, then its next place
+    uint32_t* next = lds;          // [E]: pairs of the expert, then the tile's next place
+    uint32_t* before = lds + E;    // [E]: pairs in the tiles before
+    uint32_t* hist = lds + 2 * E;  // [waves][E]: pairs of the wave, then its next place
+    uint32_t* mine = hist + w * E;
+    const int64_t p0 = blockIdx.x * tile, p1 = p0 + tile < P ? p0 + tile : P;
+    const int64_t round = (int64_t)waves * 64 * kChunks;
+
+    uint32_t e[kChunks];
+    int32_t at[kChunks];  // pos of the pairs
+    const auto load = [&](int64_t b) {
+        const int64_t p = b + w * (64 * kChunks) + lane;
+#pragma unroll
+        for (int k = 0; k < kChunks; ++k) e[k] = p + k * 64 < p1 ? (uint32_t)topk[p + k * 64] : ~0u;
+#pragma unroll
+        for (int k = 0; k < kChunks; ++k)
+            at[k] = pos && p + k * 64 < p1 ? pos[p + k * 64] : (int32_t)(p + k * 64);
+    };
+    const auto count = [&] {
+#pragma unroll
+        for (int k = 0; k < kChunks; ++k)
+            if (e[k] < (uint32_t)E) atomicAdd(mine + e[k], 1u);
+    };
+    load(p0);
     for (int i = threadIdx.x; i < (waves + 2) * E; i += blockDim.x) lds[i] = 0;
     __syncthreads();
-    const int64_t p0 = blockIdx.x * tile, p1 = p0 + tile < P ? p0 + tile : P;
-    const int64_t seg = ((p1 - p0 + waves - 1) / waves + 63) / 64 * 64;
-    const int64_t s0 = p0 + w * seg, s1 = s0 + seg < p1 ? s0 + seg : p1;
-    uint32_t* mine = hist + (int64_t)w * E;
-    for (int64_t p = s0 + lane; p < s1; p += 64) {
-        const uint32_t e = (uint32_t)topk[p];
-        if (e < (uint32_t)E) atomicAdd(mine + e, 1u);
-    }
-    if (tiles > 1) {
+    if (!kOne) {
         const int n = tiles * E, mid = blockIdx.x * E;
         for (int i = threadIdx.x; i < n; i += blockDim.x) {
             const uint32_t c = counts[i];
             if (c == 0) continue;
-            const int e = i % E;
-            atomicAdd(total + e, c);
-            if (i < mid) atomicAdd(before + e, c);
+            atomicAdd(next + i % E, c);
+            if (i < mid) atomicAdd(before + i % E, c);
         }
+    } else {
+        // the rounds behind the first, whose pairs the waves count anyway
+        for (int64_t p = p0 + round + threadIdx.x; p < p1; p += blockDim.x)
+            if ((uint32_t)topk[p] < (uint32_t)E) atomicAdd(next + topk[p], 1u);
     }
+    count();
     __syncthreads();
     // first place of each expert: each thread sums a run of experts, the runs
     // are scanned over the workgroup
     const int per = (E + blockDim.x - 1) / blockDim.x;
     const int e0 = min((int)threadIdx.x * per, E), e1 = min(e0 + per, E);
     uint32_t sum = 0;
-    for (int e = e0; e < e1; ++e) {
-        if (tiles == 1) {
-            uint32_t c = 0;
-            for (int v = 0; v < waves; ++v) c += hist[v * E + e];
-            total[e] = c;
+    for (int i = e0; i < e1; ++i) {
+        uint32_t c = next[i];
+        if (kOne) {
+            for (int v = 0; v < waves; ++v) c += hist[v * E + i];
+            next[i] = c;
         }
-        sum += total[e];
+        sum += c;
     }
     uint32_t incl = sum;
+#pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
         const uint32_t up = __shfl_up(incl, o, 64);
         if (lane >= o) incl += up;
     }
     if (lane == 63) wave_sum[w] = incl;
     __syncthreads();
-    uint32_t first = incl - sum;
-    for (int v = 0; v < w; ++v) first += wave_sum[v];
-    for (int e = e0; e < e1; ++e) {
-        const uint32_t c = total[e];
-        if (blockIdx.x == 0) offsets[e] = (int32_t)first;
-        uint32_t next = first + before[e];
-        for (int v = 0; v < waves; ++v) {
-            const uint32_t n = hist[v * E + e];
-            hist[v * E + e] = next;
-            next += n;
-        }
+    uint32_t first = incl - sum, placed = 0;
+    for (int v = 0; v < waves; ++v) {
+        first += v < w ? wave_sum[v] : 0u;
+        placed += wave_sum[v];
+    }
+    for (int i = e0; i < e1; ++i) {
+        const uint32_t c = next[i];
+        if (blockIdx.x == 0) offsets[i] = (int32_t)first;
+        next[i] = first + before[i];
         first += c;
     }
-    uint32_t placed = 0;
-    for (int v = 0; v < waves; ++v) placed += wave_sum[v];
     if (blockIdx.x == 0 && threadIdx.x == 0) offsets[E] = (int32_t)placed;
-    __syncthreads();
-    for (int64_t b = s0; b < s1; b += 64) {
-        const int64_t p = b + lane;
-        const uint32_t e = p < s1 ? (uint32_t)topk[p] : ~0u;
-        const bool valid = e < (uint32_t)E;
-        uint64_t peers = __ballot(valid);
-        for (int k = 0; k < ebits; ++k) {
-            const uint64_t bal = __ballot((e >> k) & 1u);
-            peers &= (e >> k) & 1u ? bal : ~bal;
+
+    for (int64_t b = p0;;) {
+        for (int i = e0; i < e1; ++i) {
+            uint32_t to = next[i];
+            for (int v = 0; v < waves; ++v) {
+                const uint32_t n = hist[v * E + i];
+                hist[v * E + i] = to;
+                to += n;
+            }
+            next[i] = to;
         }
-        if (valid) {
-            const int rank = __popcll(peers & ((uint64_t(1) << lane) - 1));
-            const uint32_t at = mine[e] + rank;
-            if (rank == 0) mine[e] += __popcll(peers);
-            rows[at] = pos ? pos[p] : (int32_t)p;
-            if (tokens) tokens[at] = (int32_t)((uint32_t)p / (uint32_t)K);
+        __syncthreads();
+        const int64_t p = b + w * (64 * kChunks) + lane;
+#pragma unroll
+        for (int k = 0; k < kChunks; ++k) {
+            const bool valid = e[k] < (uint32_t)E;
+            uint64_t peers = __ballot(valid);
+            if (peers == 0) continue;
+            for (int i = 0; i < ebits; ++i) {
+                const uint64_t bal = __ballot((e[k] >> i) & 1u);
+                peers &= (e[k] >> i) & 1u ? bal : ~bal;
+            }
+            if (valid) {
+                const int rank = __popcll(peers & ((uint64_t(1) << lane) - 1));
+                const uint32_t to = mine[e[k]] + rank;
+                if (rank == 0) mine[e[k]] += __popcll(peers);
+                rows[to] = at[k];
+                if (tokens) tokens[to] = (int32_t)((uint32_t)(p + k * 64) / (uint32_t)K);
+            }
         }
+        b += round;
+        if (b >= p1) break;
+        load(b);
+        __syncthreads();
+        for (int i = threadIdx.x; i < waves * E; i += blockDim.x) hist[i] = 0;
+        __syncthreads();
+        count();
+        __syncthreads();
     }
     // places behind the last pair
-    for (int64_t i = p0 + threadIdx.x; i < p1; i += blockDim.x) {
-        if (i < placed) continue;
+    for (int64_t i = max(p0, (int64_t)placed) + threadIdx.x; i < p1; i += blockDim.x) {
         rows[i] = -1;
         if (tokens) tokens[i] = -1;
     }
@@ -171,8 +213,9 @@ cobalt_status launch_expert_group(const int32_t* topk, const int32_t* pos, int64
         count_kernel<<<c.tiles, 1024, (size_t)E * 4, s>>>(topk, P, E, c.tile, (uint32_t*)ws);
         COBALT_LAUNCH_CHECK();
     }
-    place_kernel<<<c.tiles, c.waves * 64, c.lds, s>>>(topk, pos, P, K, E, ebits, c.tile, c.tiles,
-                                                      (const uint32_t*)ws, rows, tokens, offsets);
+    const auto place = c.tiles > 1 ? place_kernel<false> : place_kernel<true>;
+    place<<<c.tiles, c.waves * 64, c.lds, s>>>(topk, pos, P, K, E, ebits, c.tile, c.tiles,
+                                               (const uint32_t*)ws, rows, tokens, offsets);
     COBALT_LAUNCH_CHECK();
     return COBALT_OK;
 }

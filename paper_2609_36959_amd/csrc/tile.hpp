@@ -627,12 +627,14 @@ cobalt_status over_tiles(int64_t all, F&& kernel) {
 //   gate_up    1018 rows,  16 experts,  512 x  256:    23 |   19 |   12 |   10
 struct Choice {
     int64_t tiles;
-    int per_cu;   // workgroups that fit on a CU
-    double work;  // of a tile
-    double cost() const {
+    int per_cu;    // workgroups that fit on a CU
+    double work;   // of a step of a tile
+    double begin;  // steps that beginning and ending a tile takes the time of
+    double cost(double steps) const {
         constexpr int64_t kCus = 256;
         const int64_t side = std::max<int64_t>(1, std::min<int64_t>(per_cu, tiles / kCus + 1));
-        return (double)((tiles + kCus * side - 1) / (kCus * side)) * side * work;
+        return (double)((tiles + kCus * side - 1) / (kCus * side)) * side * work *
+               (steps + begin);
     }
 };
 // Tiles that M places of E experts are expected to make: half a tile more
@@ -645,22 +647,25 @@ inline int64_t expected_tiles(const Groups& g, int BM) {
 // values, or columns.
 enum class Along { kRows, kMxRows, kColumns };
 
-// Calls f(shape) with the shape whose count(shape) tiles cost least.
+// Calls f(shape) with the shape whose count(shape) tiles of so many steps cost
+// least. (Where the rows are k, tiles differ in their steps, and the results
+// take about as long as the products: beginning counts as nothing there.)
 template <Along kAlong, typename C, typename F>
-cobalt_status by_shape(C&& count, F&& f) {
+cobalt_status by_shape(int64_t steps, C&& count, F&& f) {
+    constexpr double kBegin = kAlong == Along::kColumns ? 0.0 : 2.0;
     const Shape<2, 2> small;
-    const Choice few{count(small), 3, 1.95};
+    const double a = Choice{count(small), 3, 1.95, kBegin}.cost(steps);
     if constexpr (kAlong == Along::kMxRows) {
         const Shape<4, 4> middle;
         const Shape<4, 6> large;
-        const double a = few.cost(), b = Choice{count(middle), 1, 4.6}.cost(),
-                     c = Choice{count(large), 1, 6.0}.cost();
+        const double b = Choice{count(middle), 1, 4.6, kBegin + 1}.cost(steps),
+                     c = Choice{count(large), 1, 6.0, kBegin + 1}.cost(steps);
         return c <= a && c <= b ? f(large) : b <= a ? f(middle) : f(small);
     } else {
         const Shape<4, 2> low;
         const Shape<4, 8> large;
-        const double a = few.cost(), b = Choice{count(low), 2, 2.8}.cost(),
-                     c = Choice{count(large), 1, 8.0}.cost();
+        const double b = Choice{count(low), 2, 2.8, kBegin}.cost(steps),
+                     c = Choice{count(large), 1, 8.0, kBegin * 1.5}.cost(steps);
         const auto others = [&] {
             return c <= a && c <= b ? f(large) : b <= a ? f(low) : f(small);
         };
@@ -668,15 +673,16 @@ cobalt_status by_shape(C&& count, F&& f) {
             return others();
         } else {
             const Shape<2, 6> high;
-            const double d = Choice{count(high), 2, 3.25}.cost();
+            const double d = Choice{count(high), 2, 3.35, kBegin}.cost(steps);
             return d < a && d < b && d < c ? f(high) : others();
         }
     }
 }
 // The same for n columns of the experts' places.
 template <Along kAlong, typename F>
-cobalt_status by_shape(const Groups& g, int64_t n, F&& f) {
+cobalt_status by_shape(const Groups& g, int64_t n, int64_t steps, F&& f) {
     return by_shape<kAlong>(
+        steps,
         [&](auto shape) {
             typedef decltype(shape) S;
             return expected_tiles(g, S::kBM) * ((n + S::kBN - 1) / S::kBN);
