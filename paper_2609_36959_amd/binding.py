@@ -9,7 +9,6 @@ built, every call raises; there is no fallback path.
 from __future__ import annotations
 
 import ctypes
-import math
 import os
 from typing import Optional
 
@@ -429,17 +428,17 @@ def cobalt_expert_gate_up_backward(dgate_up: torch.Tensor, x: Optional[torch.Ten
 def cobalt_mx_quantize(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor,
                        stream=None) -> None:
     """x [..., n] bf16 -> codes [..., n / 2], scales [..., n / 32] uint8."""
-    *lead, n = x.shape
-    _call("cobalt_mx_quantize", _dev(x, "x", BF16), math.prod(lead), n,
-          _dev(codes, "codes", U8, (*lead, n // 2)), _dev(scales, "scales", U8, (*lead, n // 32)),
-          _stream(stream))
+    lead, n = x.shape[:-1], x.shape[-1]
+    _call("cobalt_mx_quantize", _dev(x, "x", BF16), lead.numel(), n,
+          _dev(codes, "codes", U8, lead + (n // 2,)),
+          _dev(scales, "scales", U8, lead + (n // 32,)), _stream(stream))
 
 
 def cobalt_mx_dequantize(codes: torch.Tensor, scales: torch.Tensor, y: torch.Tensor,
                          stream=None) -> None:
-    *lead, n = y.shape
-    _call("cobalt_mx_dequantize", _dev(codes, "codes", U8, (*lead, n // 2)),
-          _dev(scales, "scales", U8, (*lead, n // 32)), math.prod(lead), n, _dev(y, "y", BF16),
+    lead, n = y.shape[:-1], y.shape[-1]
+    _call("cobalt_mx_dequantize", _dev(codes, "codes", U8, lead + (n // 2,)),
+          _dev(scales, "scales", U8, lead + (n // 32,)), lead.numel(), n, _dev(y, "y", BF16),
           _stream(stream))
 
 

@@ -9,8 +9,12 @@
 namespace cobalt {
 namespace {
 
+constexpr int kAhead = 4;  // chunks of a lane loaded before the first is used
+
 // One workgroup per token, one wave per slot. A wave reads its row's chunks
-// before it writes them, so the gradient may take the rows' place.
+// before it writes them, so the gradient may take the rows' place. Rows pass
+// by the caches (each is touched once); the token's gradient is read by all
+// its waves.
 __global__ __launch_bounds__(kMaxK * 64) void combine_backward_kernel(
     const u32x4* __restrict__ dy, const u32x4* eo, const int32_t* __restrict__ pos,
     const float* __restrict__ gates, int64_t t0, int K, int64_t nch, int64_t TK, u32x4* deo,
@@ -23,25 +27,34 @@ __global__ __launch_bounds__(kMaxK * 64) void combine_backward_kernel(
     const float gate = deo ? gates[t * K + j] : 0.0f;
     float sum = 0.0f;
     if (ok) {
-        for (int64_t c = lane; c < nch; c += 64) {
-            const u32x4 g = dy[t * nch + c];
-            if (dgates) {
-                const u32x4 v = eo[(int64_t)p * nch + c];
+        const u32x4* gy = dy + t * nch;
+        const u32x4* from = eo + (int64_t)p * nch;
+        u32x4* to = deo + (int64_t)p * nch;
+        for (int64_t c0 = lane; c0 < nch; c0 += 64 * kAhead) {
+            u32x4 g[kAhead], v[kAhead];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    sum = __builtin_fmaf(__uint_as_float(g[q] << 16),
-                                         __uint_as_float(v[q] << 16), sum);
-                    sum = __builtin_fmaf(__uint_as_float(g[q] & 0xffff0000u),
-                                         __uint_as_float(v[q] & 0xffff0000u), sum);
-                }
+            for (int k = 0; k < kAhead; ++k) {
+                const int64_t c = c0 + 64 * k;
+                if (c >= nch) continue;
+                g[k] = gy[c];
+                if (dgates) v[k] = __builtin_nontemporal_load(from + c);
             }
-            if (deo) {
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                const int64_t c = c0 + 64 * k;
+                if (c >= nch) continue;
                 u32x4 o;
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    o[q] = pack_bf16_rne(gate * __uint_as_float(g[q] << 16),
-                                         gate * __uint_as_float(g[q] & 0xffff0000u));
-                deo[(int64_t)p * nch + c] = o;
+                for (int q = 0; q < 4; ++q) {
+                    const float lo = __uint_as_float(g[k][q] << 16);
+                    const float hi = __uint_as_float(g[k][q] & 0xffff0000u);
+                    if (dgates) {
+                        sum = __builtin_fmaf(lo, __uint_as_float(v[k][q] << 16), sum);
+                        sum = __builtin_fmaf(hi, __uint_as_float(v[k][q] & 0xffff0000u), sum);
+                    }
+                    o[q] = pack_bf16_rne(gate * lo, gate * hi);
+                }
+                if (deo) __builtin_nontemporal_store(o, to + c);
             }
         }
     }

@@ -64,12 +64,22 @@ __device__ __forceinline__ int find_tile(const Groups& g, int BM, uint32_t id, u
     const auto tiles = [&](int lo, int hi) {
         return hi > lo ? (uint32_t)(hi - lo + BM - 1) / (uint32_t)BM : 0u;
     };
+    // up to kHeld experts of a lane stay in registers, all loaded at once
+    constexpr int kHeld = 4;
+    int off[kHeld + 1];
     uint32_t own = 0;
-    int lo = bound(e0);
-    for (int e = e0; e < e1; ++e) {
-        const int hi = bound(e + 1);
-        own += tiles(lo, hi);
-        lo = hi;
+    if (per <= kHeld) {
+#pragma unroll
+        for (int k = 0; k <= kHeld; ++k) off[k] = bound(min(e0 + k, e1));
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k) own += tiles(off[k], off[k + 1]);
+    } else {
+        int lo = bound(e0);
+        for (int e = e0; e < e1; ++e) {
+            const int hi = bound(e + 1);
+            own += tiles(lo, hi);
+            lo = hi;
+        }
     }
     uint32_t incl = own;
 #pragma unroll
@@ -77,24 +87,36 @@ __device__ __forceinline__ int find_tile(const Groups& g, int BM, uint32_t id, u
         const uint32_t up = __shfl_up(incl, o, 64);
         if (lane >= o) incl += up;
     }
-    const uint64_t hit = __ballot(id - (incl - own) < own);
+    uint32_t left = id - (incl - own);  // the lane has the tile if left < own
+    const uint64_t hit = __ballot(left < own);
     if (hit == 0) return first >= (uint32_t)__builtin_amdgcn_readlane((int)incl, 63) ? -1 : 0;
     const int src = __ffsll((unsigned long long)hit) - 1;
-    uint32_t left =
-        id - (uint32_t)__builtin_amdgcn_readlane((int)(incl - own), src);
-    int e = src * per;
-    lo = bound(e);
-    int hi = bound(e + 1);
-    while (left >= tiles(lo, hi)) {
-        left -= tiles(lo, hi);
-        ++e;
-        lo = hi;
-        hi = bound(e + 1);
+    int e = e0, lo, hi;
+    if (per <= kHeld) {
+        lo = off[0], hi = off[1];
+#pragma unroll
+        for (int k = 1; k < kHeld; ++k) {
+            const uint32_t n = tiles(lo, hi);
+            if (left >= n && e == e0 + k - 1) {
+                left -= n;
+                e = e0 + k;
+                lo = off[k], hi = off[k + 1];
+            }
+        }
+    } else {
+        left = (uint32_t)__builtin_amdgcn_readlane((int)left, src);
+        e = src * per;
+        lo = bound(e), hi = bound(e + 1);
+        while (left >= tiles(lo, hi)) {
+            left -= tiles(lo, hi);
+            ++e;
+            lo = hi;
+            hi = bound(e + 1);
+        }
     }
-    // the same in every lane, which the compiler does not see
-    out->e = __builtin_amdgcn_readfirstlane(e);
-    out->lo = __builtin_amdgcn_readfirstlane(lo + (int)left * BM);
-    out->hi = min(__builtin_amdgcn_readfirstlane(hi), out->lo + BM);
+    out->e = __builtin_amdgcn_readlane(e, src);
+    out->lo = __builtin_amdgcn_readlane(lo + (int)left * BM, src);
+    out->hi = min(__builtin_amdgcn_readlane(hi, src), out->lo + BM);
     return 1;
 }
 

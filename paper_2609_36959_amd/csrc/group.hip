@@ -1,20 +1,20 @@
 // Pairs grouped by expert: a stable counting sort of the T*K pairs by their
 // expert, in the order in which the experts' products take their rows.
 //
-// place_kernel: a workgroup takes a tile of consecutive pairs, up to 8192 at a
-// time; each wave takes a part of them, eight pairs per lane in registers. The
-// waves count their pairs by expert in histograms of their own in LDS; the
-// first place of each (wave, expert) follows from the totals of all tiles, the
-// counts of the tiles before and those of the waves before. Then each wave
-// goes through its pairs again, 64 at a time: lanes of the same expert find
-// each other by one ballot per bit of the expert, so a pair's place is the
-// wave's next place of its expert plus the number of its peers in lower lanes.
-// No order depends on scheduling.
+// place_kernel: a workgroup takes a tile of consecutive pairs; each wave takes
+// a part of them, up to eight pairs per lane in registers. The waves count
+// their pairs by expert in histograms of their own in LDS; the first place of
+// each (wave, expert) follows from the totals of all tiles, the counts of the
+// tiles before and those of the waves before. Then each wave goes through its
+// pairs again, 64 at a time: lanes of the same expert find each other by one
+// ballot per bit of the expert, so a pair's place is the wave's next place of
+// its expert plus the number of its peers in lower lanes. No order depends on
+// scheduling.
 //
-// With one tile that is the whole call, one launch. Above, count_kernel first
-// writes the counts of every tile, [tiles][E], and each workgroup of
-// place_kernel sums them for itself (they come out of the L2): that costs less
-// than a third launch.
+// The ballots are what takes time, so pairs are spread over workgroups, 1024
+// to each. Up to kSelfPairs pairs each workgroup counts all pairs itself, which
+// costs less than a launch; beyond, count_kernel first writes the counts of
+// every tile, [tiles][E], and each workgroup sums them.
 #include <algorithm>
 
 #include "internal.hpp"
@@ -22,26 +22,28 @@
 namespace cobalt {
 namespace {
 
-constexpr int kChunks = 8;             // pairs of a lane
-constexpr int kTilePairs = 16 * 64 * kChunks;
+constexpr int kChunks = 8;             // pairs of a lane, at most
 constexpr int64_t kMaxTiles = 256;
+constexpr int64_t kSelfPairs = 65536;
 
 struct Cut {
-    int64_t tile;   // pairs of a tile
-    int tiles, waves;
+    int64_t tile;  // pairs of a tile
+    int tiles, waves, chunks;
+    bool self;
     size_t lds;
 };
 
 Cut cut_pairs(int64_t P, int E) {
     Cut c;
-    // tiles of a workgroup's registers, or as much longer as keeps them few
-    const int64_t most = (P + kMaxTiles - 1) / kMaxTiles;
-    c.tile = std::max<int64_t>((most + kTilePairs - 1) / kTilePairs * kTilePairs, kTilePairs);
+    // 1024 pairs to a tile, or as many more as keep the tiles few
+    c.tile = std::max<int64_t>(((P + kMaxTiles - 1) / kMaxTiles + 1023) / 1024, 1) * 1024;
     c.tiles = (int)std::max<int64_t>((P + c.tile - 1) / c.tile, 1);
+    c.self = P <= kSelfPairs;
     // as many waves as have pairs, and whose histograms leave room in LDS
     const int64_t want = std::min<int64_t>((P + 63) / 64, 16);
     const int64_t room = 64 * 1024 / (4 * (int64_t)E) - 2;
     c.waves = (int)std::max<int64_t>(1, std::min(want, room));
+    c.chunks = (int)std::min<int64_t>((c.tile + c.waves * 64 - 1) / (c.waves * 64), kChunks);
     c.lds = (size_t)(c.waves + 2) * E * 4;
     return c;
 }
@@ -66,11 +68,11 @@ __global__ __launch_bounds__(1024) void count_kernel(const int32_t* __restrict__
     for (int e = threadIdx.x; e < E; e += 1024) counts[(int64_t)blockIdx.x * E + e] = hist[e];
 }
 
-// kOne: one tile, whose totals it counts itself.
-template <bool kOne>
+// kSelf: without the counts of another kernel.
+template <bool kSelf>
 __global__ __launch_bounds__(1024) void place_kernel(
     const int32_t* __restrict__ topk, const int32_t* __restrict__ pos, int64_t P, int K, int E,
-    int ebits, int64_t tile, int tiles, const uint32_t* __restrict__ counts,
+    int ebits, int64_t tile, int tiles, int chunks, const uint32_t* __restrict__ counts,
     int32_t* __restrict__ rows, int32_t* __restrict__ tokens, int32_t* __restrict__ offsets) {
     extern __shared__ uint32_t lds[];
     __shared__ uint32_t wave_sum[16];
@@ -80,17 +82,18 @@ __global__ __launch_bounds__(1024) void place_kernel(
     uint32_t* hist = lds + 2 * E;  // [waves][E]: pairs of the wave, then its next place
     uint32_t* mine = hist + w * E;
     const int64_t p0 = blockIdx.x * tile, p1 = p0 + tile < P ? p0 + tile : P;
-    const int64_t round = (int64_t)waves * 64 * kChunks;
+    const int64_t round = (int64_t)waves * 64 * chunks;
 
     uint32_t e[kChunks];
     int32_t at[kChunks];  // pos of the pairs
     const auto load = [&](int64_t b) {
-        const int64_t p = b + w * (64 * kChunks) + lane;
-#pragma unroll
-        for (int k = 0; k < kChunks; ++k) e[k] = p + k * 64 < p1 ? (uint32_t)topk[p + k * 64] : ~0u;
+        const int64_t p = b + w * (64 * chunks) + lane;
 #pragma unroll
         for (int k = 0; k < kChunks; ++k)
-            at[k] = pos && p + k * 64 < p1 ? pos[p + k * 64] : (int32_t)(p + k * 64);
+            e[k] = k < chunks && p + k * 64 < p1 ? (uint32_t)topk[p + k * 64] : ~0u;
+#pragma unroll
+        for (int k = 0; k < kChunks; ++k)
+            if (k < chunks && p + k * 64 < p1) at[k] = pos ? pos[p + k * 64] : (int32_t)(p + k * 64);
     };
     const auto count = [&] {
 #pragma unroll
@@ -100,7 +103,23 @@ __global__ __launch_bounds__(1024) void place_kernel(
     load(p0);
     for (int i = threadIdx.x; i < (waves + 2) * E; i += blockDim.x) lds[i] = 0;
     __syncthreads();
-    if (!kOne) {
+    if (kSelf) {
+        constexpr int kAtOnce = 8;
+        for (int64_t b = threadIdx.x; b < P; b += (int64_t)blockDim.x * kAtOnce) {
+            uint32_t v[kAtOnce];
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) {
+                const int64_t p = b + (int64_t)k * blockDim.x;
+                v[k] = p < P ? (uint32_t)topk[p] : ~0u;
+            }
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) {
+                if (v[k] >= (uint32_t)E) continue;
+                atomicAdd(next + v[k], 1u);
+                if (b + (int64_t)k * blockDim.x < p0) atomicAdd(before + v[k], 1u);
+            }
+        }
+    } else {
         const int n = tiles * E, mid = blockIdx.x * E;
         for (int i = threadIdx.x; i < n; i += blockDim.x) {
             const uint32_t c = counts[i];
@@ -108,10 +127,6 @@ __global__ __launch_bounds__(1024) void place_kernel(
             atomicAdd(next + i % E, c);
             if (i < mid) atomicAdd(before + i % E, c);
         }
-    } else {
-        // the rounds behind the first, whose pairs the waves count anyway
-        for (int64_t p = p0 + round + threadIdx.x; p < p1; p += blockDim.x)
-            if ((uint32_t)topk[p] < (uint32_t)E) atomicAdd(next + topk[p], 1u);
     }
     count();
     __syncthreads();
@@ -120,14 +135,7 @@ __global__ __launch_bounds__(1024) void place_kernel(
     const int per = (E + blockDim.x - 1) / blockDim.x;
     const int e0 = min((int)threadIdx.x * per, E), e1 = min(e0 + per, E);
     uint32_t sum = 0;
-    for (int i = e0; i < e1; ++i) {
-        uint32_t c = next[i];
-        if (kOne) {
-            for (int v = 0; v < waves; ++v) c += hist[v * E + i];
-            next[i] = c;
-        }
-        sum += c;
-    }
+    for (int i = e0; i < e1; ++i) sum += next[i];
     uint32_t incl = sum;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -160,7 +168,7 @@ __global__ __launch_bounds__(1024) void place_kernel(
             next[i] = to;
         }
         __syncthreads();
-        const int64_t p = b + w * (64 * kChunks) + lane;
+        const int64_t p = b + w * (64 * chunks) + lane;
 #pragma unroll
         for (int k = 0; k < kChunks; ++k) {
             const bool valid = e[k] < (uint32_t)E;
@@ -196,10 +204,13 @@ __global__ __launch_bounds__(1024) void place_kernel(
 
 }  // namespace
 
-// The counts of every tile. Fewer pairs never take more tiles.
+// The counts of every tile; more pairs never take fewer tiles than 256 once
+// they have as many, and the size is theirs for all calls that large.
 size_t expert_group_workspace_bytes(int64_t T, int K, int E) {
-    const Cut c = cut_pairs(T * K, E);
-    return std::max<size_t>(((size_t)c.tiles * E * 4 + 255) / 256 * 256, 256);
+    const int64_t P = T * K;
+    if (P <= kSelfPairs) return 256;
+    const int64_t tiles = std::min<int64_t>((P + 1023) / 1024, kMaxTiles);
+    return ((size_t)tiles * E * 4 + 255) / 256 * 256;
 }
 
 cobalt_status launch_expert_group(const int32_t* topk, const int32_t* pos, int64_t T, int K, int E,
@@ -209,13 +220,14 @@ cobalt_status launch_expert_group(const int32_t* topk, const int32_t* pos, int64
     const Cut c = cut_pairs(P, E);
     int ebits = 0;
     while ((1 << ebits) < E) ++ebits;
-    if (c.tiles > 1) {
+    if (!c.self) {
         count_kernel<<<c.tiles, 1024, (size_t)E * 4, s>>>(topk, P, E, c.tile, (uint32_t*)ws);
         COBALT_LAUNCH_CHECK();
     }
-    const auto place = c.tiles > 1 ? place_kernel<false> : place_kernel<true>;
+    const auto place = c.self ? place_kernel<true> : place_kernel<false>;
     place<<<c.tiles, c.waves * 64, c.lds, s>>>(topk, pos, P, K, E, ebits, c.tile, c.tiles,
-                                               (const uint32_t*)ws, rows, tokens, offsets);
+                                               c.chunks, (const uint32_t*)ws, rows, tokens,
+                                               offsets);
     COBALT_LAUNCH_CHECK();
     return COBALT_OK;
 }
