@@ -18,54 +18,18 @@ constexpr int kFewPlaces = 16;  // places of a tile
 constexpr int kFewWaves = 8;    // waves of a workgroup
 constexpr int kAhead = 4, kLeast = 8;
 
-// A lane's chunk of a fragment, with its scale where there are scales.
-struct Bf16Chunk {
-    u32x4 v;
-    template <typename Side>
-    __device__ __forceinline__ void load(const Side& s, int64_t row, int c) {
-        v = *(const u32x4*)(s.row(row) + c * 16);
-    }
-    __device__ __forceinline__ void clear() { v = u32x4{0, 0, 0, 0}; }
-    __device__ __forceinline__ static f32x4 product(const Bf16Chunk& p, const Bf16Chunk& q,
-                                                    const f32x4& c) {
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, p.v),
-                                                       __builtin_bit_cast(bf16x8, q.v), c, 0, 0,
-                                                       0);
-    }
-};
-struct MxChunk {
-    u32x4 v;
-    int scale;
-    template <typename Side>
-    __device__ __forceinline__ void load(const Side& s, int64_t row, int c) {
-        v = *(const u32x4*)(s.row(row) + c * 16);
-        scale = (uint8_t)s.scale_row(row)[c];
-    }
-    __device__ __forceinline__ void clear() {
-        v = u32x4{0, 0, 0, 0};
-        scale = 0;
-    }
-    __device__ __forceinline__ static f32x4 product(const MxChunk& p, const MxChunk& q,
-                                                    const f32x4& c) {
-        return mx_product<0, 0>(__builtin_bit_cast(bf16x8, p.v), __builtin_bit_cast(bf16x8, q.v),
-                                c, p.scale, q.scale);
-    }
-};
-
 // sums[part][group][s][m][n] of the workgroup's waves: S weight rows per lane,
-// row[s] of w, times place row `at` of x (-1: weights in its place).
-template <int KS, int S, typename Side>
-__device__ __forceinline__ void stream_products(float* sums, const Side& x, int64_t at,
-                                                const Side& w, const int64_t (&row)[S]) {
-    typedef std::conditional_t<Side::kScaled, MxChunk, Bf16Chunk> Chunk;
+// row[s] of w, times row `at` of x (-1: weights in its place).
+template <int KS, int S, bool kWhole>
+__device__ __forceinline__ void stream_products(float* sums, const Bf16Rows<kWhole>& x, int64_t at,
+                                                const Bf16Rows<kWhole>& w,
+                                                const int64_t (&row)[S]) {
     const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4, wv = wave_id();
     const int chunks = (int)(w.bytes / 16), steps = (chunks + 3) / 4;
     const int per = (steps + KS - 1) / KS, part = wv % KS;
     const int s0 = part * per, s1 = min(s0 + per, steps);
-    const bool none = at < 0;
-    const Side& from = none ? w : x;
-    const int64_t q_row = none ? row[0] : at;
-    Chunk p[2][kAhead][S], q[2][kAhead];
+    const char* q_row = at < 0 ? w.row(row[0]) : x.row(at);
+    u32x4 p[2][kAhead][S], q[2][kAhead];
     f32x4 acc[S];
 #pragma unroll
     for (int k = 0; k < S; ++k) acc[k] = f32x4{0, 0, 0, 0};
@@ -75,24 +39,27 @@ __device__ __forceinline__ void stream_products(float* sums, const Side& x, int6
         for (int a = 0; a < kAhead; ++a) {
             const int c = min((s + a) * 4 + g, chunks - 1);
 #pragma unroll
-            for (int k = 0; k < S; ++k) p[to][a][k].load(w, row[k], c);
+            for (int k = 0; k < S; ++k) p[to][a][k] = *(const u32x4*)(w.row(row[k]) + c * 16);
         }
 #pragma unroll
         for (int a = 0; a < kAhead; ++a)
-            q[to][a].load(from, q_row, min((s + a) * 4 + g, chunks - 1));
+            q[to][a] = *(const u32x4*)(q_row + min((s + a) * 4 + g, chunks - 1) * 16);
         __builtin_amdgcn_sched_barrier(0);
     };
     const auto multiply = [&](int of, int s) {
 #pragma unroll
         for (int a = 0; a < kAhead; ++a) {
             if (s + a >= s1) break;
-            if (!Side::kWhole && (s + a) * 4 + g >= chunks) {
-                q[of][a].clear();
+            if (!kWhole && (s + a) * 4 + g >= chunks) {
+                q[of][a] = u32x4{0, 0, 0, 0};
 #pragma unroll
-                for (int k = 0; k < S; ++k) p[of][a][k].clear();
+                for (int k = 0; k < S; ++k) p[of][a][k] = u32x4{0, 0, 0, 0};
             }
 #pragma unroll
-            for (int k = 0; k < S; ++k) acc[k] = Chunk::product(p[of][a][k], q[of][a], acc[k]);
+            for (int k = 0; k < S; ++k)
+                acc[k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                    __builtin_bit_cast(bf16x8, p[of][a][k]), __builtin_bit_cast(bf16x8, q[of][a]),
+                    acc[k], 0, 0, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
     };
@@ -181,8 +148,17 @@ cobalt_status by_parts(int64_t bytes, F&& f) {
     return f(std::integral_constant<int, 1>());
 }
 
-// Whether the products of M places of E experts stream the weights.
-inline bool few_rows(const Groups& g) { return g.M <= 16 * (int64_t)g.E; }
+// Whether products with n weight rows stream the weights: while tiles of 64 x
+// 128 would leave CUs without work, whose loads of a step then wait for the
+// step before. With experts of 4096 x 1024 out of memory, in us, streamed | in
+// tiles:
+//   places      1           4           8          16          64
+//   gate_up  13 |  35    16 |  45    30 |  57    52 |  60    99 |  86
+//   down      7 |  11    10 |  13    18 |  18    31 |  22    63 |  50
+// (4-bit products take as long in tiles from one place on.)
+inline bool few_rows(const Groups& g, int64_t n) {
+    return expected_tiles(g, 64) * tiles(n, 128) <= 256;
+}
 
 // Workgroups for n columns.
 inline int64_t few_grid(const Groups& g, int64_t n, int ks) {
@@ -193,14 +169,15 @@ template <typename Side>
 cobalt_status gate_up(const Groups& g, const Side& x, Rows rows, const Side& w, int64_t f, Act act,
                       void* h, void* gu, hipStream_t s) {
     return by_act(act, [&](auto a) {
-        if (few_rows(g))
-            return by_parts(w.bytes, [&](auto ks) {
-                return over_tiles<false>(
-                    few_grid(g, f, ks()), [&](uint32_t b0, unsigned n, uint32_t) {
-                        gate_up_few_kernel<ks(), a(), Side><<<n, 512, 0, s>>>(
-                            g, b0, x, rows, w, f, (uint16_t*)h, (uint16_t*)gu);
-                    });
-            });
+        if constexpr (!Side::kScaled)
+            if (few_rows(g, f * 2))
+                return by_parts(w.bytes, [&](auto ks) {
+                    return over_tiles<false>(
+                        few_grid(g, f, ks()), [&](uint32_t b0, unsigned n, uint32_t) {
+                            gate_up_few_kernel<ks(), a(), Side><<<n, 512, 0, s>>>(
+                                g, b0, x, rows, w, f, (uint16_t*)h, (uint16_t*)gu);
+                        });
+                });
         return by_shape<Side::kAlong>(g, f * 2, tiles(w.bytes, kStepBytes), [&](auto shape) {
             typedef decltype(shape) S;
             return over_tiles<S::kStays>(
@@ -216,14 +193,15 @@ cobalt_status gate_up(const Groups& g, const Side& x, Rows rows, const Side& w, 
 template <typename Side>
 cobalt_status down(const Groups& g, const Side& h, const Side& w, int64_t d, Rows rows, void* out,
                    hipStream_t s) {
-    if (few_rows(g))
-        return by_parts(w.bytes, [&](auto ks) {
-            return over_tiles<false>(
-                few_grid(g, d, ks()), [&](uint32_t b0, unsigned n, uint32_t) {
-                    down_few_kernel<ks(), Side>
-                        <<<n, 512, 0, s>>>(g, b0, h, w, d, rows, (uint16_t*)out);
-                });
-        });
+    if constexpr (!Side::kScaled)
+        if (few_rows(g, d))
+            return by_parts(w.bytes, [&](auto ks) {
+                return over_tiles<false>(
+                    few_grid(g, d, ks()), [&](uint32_t b0, unsigned n, uint32_t) {
+                        down_few_kernel<ks(), Side>
+                            <<<n, 512, 0, s>>>(g, b0, h, w, d, rows, (uint16_t*)out);
+                    });
+            });
     return by_shape<Side::kAlong>(g, d, tiles(w.bytes, kStepBytes), [&](auto shape) {
         typedef decltype(shape) S;
         return over_tiles<S::kStays>(

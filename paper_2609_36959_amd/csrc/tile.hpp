@@ -20,6 +20,8 @@
 // at 1.05.
 #pragma once
 
+#include <cmath>
+
 #include "experts.hpp"
 
 namespace cobalt {
@@ -30,15 +32,16 @@ typedef int16_t s16x4 __attribute__((ext_vector_type(4)));
 typedef int16_t s16x8 __attribute__((ext_vector_type(8)));
 
 // A tile of kBM x kBN results made by kWM x kWN waves, each with TM x 4 tiles
-// of 16 x 16.
-template <int WN, int TM>
+// of 16 x 16, from ST stages of LDS.
+template <int WN, int TM, int ST = 2>
 struct Shape {
+    static constexpr int kStages = ST;
     static constexpr int kWM = 2, kWN = WN, kTM = TM;
     static constexpr int kWaves = kWM * kWN, kThreads = 64 * kWaves;
     static constexpr int kBM = kWM * TM * 16, kBN = kWN * 64;
     // two or three workgroups share a CU where the stages leave room for them;
     // otherwise one stays there and goes from tile to tile
-    static constexpr bool kStays = 2 * (kBM + kBN) * 128 > 80 * 1024;
+    static constexpr bool kStays = ST * (kBM + kBN) * 128 > 80 * 1024;
 };
 constexpr int kStepBytes = 128;
 
@@ -107,15 +110,11 @@ struct RowOperand {
     }
     __device__ __forceinline__ void load(char* lds, int s) {
         const int w = wave_id();
-        if (kWhole || chunk(threadIdx.x) * 16 < bytes - (int64_t)s * kStepBytes) {
+        // behind the end of the rows: zeros, on both sides of a product
+        const bool in = kWhole || chunk(threadIdx.x) * 16 < bytes - (int64_t)s * kStepBytes;
 #pragma unroll
-            for (int j = 0; j < kLoads; ++j) load_to_lds(at(j), lds + (j * kWaves + w) * 1024);
-        } else {  // behind the end of the rows: zeros, on both sides of a product
-#pragma unroll
-            for (int j = 0; j < kLoads; ++j)
-                *(u32x4*)(lds + (j * kWaves + w) * 1024 + (threadIdx.x & 63) * 16) =
-                    u32x4{0, 0, 0, 0};
-        }
+        for (int j = 0; j < kLoads; ++j)
+            load_to_lds(in ? at(j) : (const char*)kNothing, lds + (j * kWaves + w) * 1024);
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
             if constexpr (kNear)
@@ -377,42 +376,56 @@ template <typename S, typename Math, bool kTurns>
 struct Lds {
     static constexpr int kStage = (S::kBM + S::kBN) * kStepBytes;
     static constexpr int kTurnBytes = S::kWaves * kTurn * 4;
-    static constexpr int kTiles = 2 * kStage + Math::kLds;
+    static constexpr int kTiles = S::kStages * kStage + Math::kLds;
     static constexpr int kBytes = kTiles + (kTurns && S::kStays ? kTurnBytes : 0);
-    static_assert(kTurnBytes <= 2 * kStage && kBytes <= 160 * 1024, "LDS of a CU");
+    static_assert(kTurnBytes <= kTiles && kBytes <= 160 * 1024, "LDS of a CU");
+    static_assert(Math::kLds == 0 || S::kStages == 2, "the scales have two stages");
     __device__ static char* turn(char* lds) { return lds + (S::kStays ? kTiles : 0); }
 };
 
-// The steps of a tile. issue() begins the loads of the first two into LDS,
-// which no wave reads at that time; after arrive() the wave's part of them is
-// there, and run() does the rest. Results of the tile before are stored between
+// The steps of a tile. issue() begins the loads of the first stages into LDS,
+// which no wave reads at that time; after arrive() the wave's part of the first
+// two is there, and run() does the rest. Results of the tile before are stored between
 // the two: then run() does not wait for those stores until its second step.
 template <typename S, typename Q, typename P, typename Math>
 struct Pipe {
     static constexpr int TM = S::kTM, kBM = S::kBM, kStage = (kBM + S::kBN) * kStepBytes;
+    static constexpr int kStages = S::kStages;
+    // loads that may be under way when the step after the current one has to be
+    // there: those of the stages behind it (loads end in order)
+    static constexpr int kBehind = (kStages - 2) * (Q::kLoads + P::kLoads);
     char* lds;
     Q q;
     P p;
     Math math;
 
+    __device__ __forceinline__ char* stage(int s) const { return lds + s % kStages * kStage; }
     __device__ __forceinline__ void load(int s) {
-        char* at = lds + (s & 1) * kStage;
+        char* at = stage(s);
         q.load(at, s);
         p.load(at + kBM * kStepBytes, s);
     }
     __device__ __forceinline__ void issue(int steps) {
         if (steps == 0) return;
-        load(0);
-        if (steps > 1) load(1);
+#pragma unroll
+        for (int s = 0; s < kStages; ++s)
+            if (s < steps) load(s);
         math.issue(steps);
     }
-    __device__ __forceinline__ void arrive() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+    // `full`: the loads of all stages have been issued
+    __device__ __forceinline__ static void wait(bool full) {
+        if (full)
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kBehind) : "memory");
+        else
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
+    __device__ __forceinline__ void arrive(int steps) { wait(steps >= kStages); }
     __device__ __forceinline__ void run(int steps, Acc<TM>& acc) {
         const int w = wave_id(), m0 = w / S::kWN * (TM * 16), n0 = w % S::kWN * 64;
-        char* extra = lds + 2 * kStage;
+        char* extra = lds + kStages * kStage;
         bf16x8 fq[2][TM], fp[2][4];
         const auto read = [&](int to, int s, int kk) {
-            const char* at = lds + (s & 1) * kStage;
+            const char* at = stage(s);
             if (kk == 0) math.read(extra, s);
 #pragma unroll
             for (int t = 0; t < 4; ++t) fp[to][t] = P::read(at + kBM * kStepBytes, n0, t, kk);
@@ -455,11 +468,11 @@ struct Pipe {
         for (int s = 0; s < steps; ++s) {
             half(0, s);
             // every wave has read stage s and has its part of stage s + 1
-            if (s > 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            if (s > 0) wait(s + kStages - 1 < steps);
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            if (s + 2 < steps) {
+            if (s + kStages < steps) {
                 math.commit(extra, s + 2);
-                load(s + 2);
+                load(s + kStages);
                 if (s + 3 < steps) math.prefetch();
             }
             __builtin_amdgcn_sched_barrier(0);
@@ -493,7 +506,7 @@ __device__ __forceinline__ void make_tiles(Pi& pipe, uint32_t b, uint32_t all, F
     if (!from(&job)) return;
     start(job);
     pipe.issue(job.steps);
-    pipe.arrive();
+    pipe.arrive(job.steps);
     for (;;) {
         Job next;
         bool more = false;
@@ -506,7 +519,7 @@ __device__ __forceinline__ void make_tiles(Pi& pipe, uint32_t b, uint32_t all, F
         if (more) {
             start(next);
             pipe.issue(next.steps);
-            pipe.arrive();
+            pipe.arrive(next.steps);
         }
         finish(job, acc);
         if (!more) return;
@@ -637,10 +650,12 @@ struct Choice {
                (steps + begin);
     }
 };
-// Tiles that M places of E experts are expected to make: half a tile more
-// than full ones for each expert.
+// Tiles of BM places that M places of E experts are expected to make, if every
+// expert is as likely: one for each expert with places, or half a tile more
+// than full ones.
 inline int64_t expected_tiles(const Groups& g, int BM) {
-    return g.M / BM + (std::min<int64_t>(g.E, g.M) + 1) / 2;
+    const double E = g.E, M = g.M, with = E * (1.0 - std::exp(-M / E));
+    return (int64_t)std::ceil(std::max(with, M / BM + with / 2));
 }
 
 // What the rows of a product's tiles are: rows in memory, of bf16 or 4-bit
