@@ -160,7 +160,7 @@ cobalt_status launch_down_gradient(const Groups& g, const void* dout, Rows rows,
                                    void* dgate_up, hipStream_t s) {
     return by_act(act, [&](auto a) {
         return by_bool(d % 64 == 0, [&](auto whole) {
-            return by_shape<Along::kRows>(g, f, tiles(d, 64), [&](auto shape) {
+            return by_shape<Along::kOne>(g, f, tiles(d, 64), [&](auto shape) {
                 typedef decltype(shape) S;
                 return over_tiles<S::kStays>(
                     tile_grid(most_tiles(g.M, g.E, S::kBM), tiles(f, S::kBN)),
@@ -177,7 +177,7 @@ cobalt_status launch_down_gradient(const Groups& g, const void* dout, Rows rows,
 cobalt_status launch_gate_up_gradient(const Groups& g, const void* dgate_up, int64_t d, int64_t f,
                                       const void* w_in, Rows rows, void* dx, hipStream_t s) {
     return by_bool(f % 32 == 0, [&](auto whole) {
-        return by_shape<Along::kRows>(g, d, tiles(2 * f, 64), [&](auto shape) {
+        return by_shape<Along::kOne>(g, d, tiles(2 * f, 64), [&](auto shape) {
             typedef decltype(shape) S;
             return over_tiles<S::kStays>(
                 tile_grid(most_tiles(g.M, g.E, S::kBM), tiles(d, S::kBN)),
@@ -215,7 +215,7 @@ cobalt_status launch_weight_gradient(const Groups& g, const void* a, int64_t na,
         if (!f32) return gather(shape, no, no);
         return add ? gather(shape, yes, yes) : gather(shape, yes, no);
     };
-    return by_shape<Along::kColumns>(
+    return by_shape<Along::kNeither>(
         1,
         [&](auto shape) {
             typedef decltype(shape) S;

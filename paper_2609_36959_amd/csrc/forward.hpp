@@ -12,7 +12,7 @@ struct Bf16Rows {
     template <typename S>
     using Math = Bf16Math<S>;
     static constexpr bool kScaled = false, kWhole = kW;
-    static constexpr Along kAlong = Along::kRows;
+    static constexpr Along kAlong = Along::kBoth;
     const char* v;
     int64_t bytes;
     __host__ __device__ Bf16Rows(const void* p, const void*, int64_t n)
@@ -25,7 +25,7 @@ struct MxRows {
     template <typename S>
     using Math = MxMath<S, kW>;
     static constexpr bool kScaled = true, kWhole = kW;
-    static constexpr Along kAlong = Along::kMxRows;
+    static constexpr Along kAlong = Along::kMxBoth;
     const char* v;
     const char* s;
     int64_t bytes, scales;

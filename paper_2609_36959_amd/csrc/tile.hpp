@@ -1,23 +1,25 @@
 // Tiles of the experts' products on the matrix cores.
 //
-// A workgroup of eight waves makes a tile of BM x 256 results, acc[m][n] =
-// sum_k q(m, k) p(n, k), in fp32. The operands pass through LDS in steps of
-// 128 bytes of k per row (64 bf16 values, or 256 of 4 bits), two stages. Per
-// step and wave there are two halves; each multiplies what the half before
-// has read from LDS into registers and reads what the next one needs, one
-// read between every few products, so that the matrix cores and LDS work at
-// the same time. In the middle of a step every wave has read all of its
+// A workgroup of four or eight waves makes a tile of BM x BN results,
+// acc[m][n] = sum_k q(m, k) p(n, k), in fp32. The operands pass through LDS in
+// steps of 128 bytes of k per row (64 bf16 values, or 256 of 4 bits), two
+// stages. Per step and wave there are two halves; each multiplies what the half
+// before has read from LDS into registers and reads what the next one needs,
+// one read between every few products, so that the matrix cores and LDS work
+// at the same time. In the middle of a step every wave has read all of its
 // stage: one barrier there frees the stage, and the loads of the step after
-// the next go straight into it (global to LDS, no registers), a whole step
-// before they are waited for.
+// the next go straight into it (global to LDS, no registers) among the second
+// half's products, nearly a step before they are waited for.
 //
 // Results are transposed on the matrix cores: p is the operand of their rows,
 // so that a lane holds consecutive n of one m and stores whole vectors.
 //
-// On 8192^3 the loop reaches 1.29 PFLOP/s, and 1.31 on 16384 x 4096 x 7168
-// (a library product of the same operands 1.32 and 1.28 in that run); four
-// waves with 128 x 128 results each, which read a third less from LDS, stay
-// at 1.05.
+// Bound by the matrix cores at the clock that the card's power leaves them:
+// 16384 x 4096 x 7168 as 8 experts' gate and up projections takes 897 us,
+// 1.07 PFLOP/s, with 192 x 128 tiles (a library product of one such matrix 0.60
+// to 0.75 ms); a single expert's 8192^3 runs at 1.3 PFLOP/s, as the library's. Three and four stages instead of two gained
+// nothing, and four waves with 128 x 128 results each, which read a third less
+// from LDS, stay at 1.05.
 #pragma once
 
 #include <cmath>
@@ -32,16 +34,15 @@ typedef int16_t s16x4 __attribute__((ext_vector_type(4)));
 typedef int16_t s16x8 __attribute__((ext_vector_type(8)));
 
 // A tile of kBM x kBN results made by kWM x kWN waves, each with TM x 4 tiles
-// of 16 x 16, from ST stages of LDS.
-template <int WN, int TM, int ST = 2>
+// of 16 x 16.
+template <int WN, int TM>
 struct Shape {
-    static constexpr int kStages = ST;
     static constexpr int kWM = 2, kWN = WN, kTM = TM;
     static constexpr int kWaves = kWM * kWN, kThreads = 64 * kWaves;
     static constexpr int kBM = kWM * TM * 16, kBN = kWN * 64;
     // two or three workgroups share a CU where the stages leave room for them;
     // otherwise one stays there and goes from tile to tile
-    static constexpr bool kStays = ST * (kBM + kBN) * 128 > 80 * 1024;
+    static constexpr bool kStays = 2 * (kBM + kBN) * 128 > 80 * 1024;
 };
 constexpr int kStepBytes = 128;
 
@@ -376,30 +377,30 @@ template <typename S, typename Math, bool kTurns>
 struct Lds {
     static constexpr int kStage = (S::kBM + S::kBN) * kStepBytes;
     static constexpr int kTurnBytes = S::kWaves * kTurn * 4;
-    static constexpr int kTiles = S::kStages * kStage + Math::kLds;
+    static constexpr int kTiles = 2 * kStage + Math::kLds;
     static constexpr int kBytes = kTiles + (kTurns && S::kStays ? kTurnBytes : 0);
     static_assert(kTurnBytes <= kTiles && kBytes <= 160 * 1024, "LDS of a CU");
-    static_assert(Math::kLds == 0 || S::kStages == 2, "the scales have two stages");
     __device__ static char* turn(char* lds) { return lds + (S::kStays ? kTiles : 0); }
 };
 
-// The steps of a tile. issue() begins the loads of the first stages into LDS,
-// which no wave reads at that time; after arrive() the wave's part of the first
-// two is there, and run() does the rest. Results of the tile before are stored between
+// The steps of a tile. issue() begins the loads of the first two stages into
+// LDS, which no wave reads at that time; after arrive() the wave's part of them
+// is there, and run() does the rest. Results of the tile before are stored between
 // the two: then run() does not wait for those stores until its second step.
 template <typename S, typename Q, typename P, typename Math>
 struct Pipe {
     static constexpr int TM = S::kTM, kBM = S::kBM, kStage = (kBM + S::kBN) * kStepBytes;
-    static constexpr int kStages = S::kStages;
-    // loads that may be under way when the step after the current one has to be
-    // there: those of the stages behind it (loads end in order)
-    static constexpr int kBehind = (kStages - 2) * (Q::kLoads + P::kLoads);
+    // Whether the loads of a stage are issued among products. 256 x 256 tiles
+    // have no registers left for it: 391 us become 411 for the gradient of
+    // weights 64 x 2048 x 2048 of 24576 rows, 161 us 183 for their output
+    // projection. All others gain 1 to 7 %.
+    static constexpr bool kAmong = TM < 8;
     char* lds;
     Q q;
     P p;
     Math math;
 
-    __device__ __forceinline__ char* stage(int s) const { return lds + s % kStages * kStage; }
+    __device__ __forceinline__ char* stage(int s) const { return lds + s % 2 * kStage; }
     __device__ __forceinline__ void load(int s) {
         char* at = stage(s);
         q.load(at, s);
@@ -407,22 +408,16 @@ struct Pipe {
     }
     __device__ __forceinline__ void issue(int steps) {
         if (steps == 0) return;
-#pragma unroll
-        for (int s = 0; s < kStages; ++s)
-            if (s < steps) load(s);
+        load(0);
+        if (steps > 1) load(1);
         math.issue(steps);
     }
-    // `full`: the loads of all stages have been issued
-    __device__ __forceinline__ static void wait(bool full) {
-        if (full)
-            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kBehind) : "memory");
-        else
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __device__ __forceinline__ static void arrive() {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
-    __device__ __forceinline__ void arrive(int steps) { wait(steps >= kStages); }
     __device__ __forceinline__ void run(int steps, Acc<TM>& acc) {
         const int w = wave_id(), m0 = w / S::kWN * (TM * 16), n0 = w % S::kWN * 64;
-        char* extra = lds + kStages * kStage;
+        char* extra = lds + 2 * kStage;
         bf16x8 fq[2][TM], fp[2][4];
         const auto read = [&](int to, int s, int kk) {
             const char* at = stage(s);
@@ -432,21 +427,36 @@ struct Pipe {
 #pragma unroll
             for (int t = 0; t < TM; ++t) fq[to][t] = Q::read(at, m0, t, kk);
         };
-        // the products of half kk, and the reads of the half after it
-        const auto half = [&](int kk, int s) {
+        // the products of half kk, the reads of the half after it and, with
+        // kLoad, the loads of stage s + 2
+        const auto half = [&](auto load_too, int kk, int s) {
+            constexpr bool kLoad = load_too() && kAmong;
+            if constexpr (kLoad) load(s + 2);
             read(kk ^ 1, s + kk, kk ^ 1);
 #pragma unroll
             for (int x = 0; x < TM; ++x)
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
                     acc[x][t] = math.product(fp[kk][t], fq[kk][x], acc[x][t], x, t, kk);
-            constexpr int kR = TM * Q::kReads + 4 * P::kReads + Math::kReads, kM = 4 * TM;
+            // Loads with a product before each: a wave that issues its loads at
+            // once has no product to offer while the CU takes them, 64 bytes a
+            // cycle. Then products before each read: the first products wait
+            // for the reads of the half before, and would for one of this half,
+            // too.
+            constexpr int kV = kLoad ? Q::kLoads + P::kLoads : 0;
+            constexpr int kR = TM * Q::kReads + 4 * P::kReads + Math::kReads, kM = 4 * TM - kV;
             constexpr int kPer = kM / kR > 0 ? kM / kR : 1;
             constexpr int kGroups = kM / kPer < kR ? kM / kPer : kR;
 #pragma unroll
+            for (int i = 0; i < kV; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // a product
+                __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);  // a load
+            }
+#pragma unroll
             for (int i = 0; i < kGroups; ++i) {
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);     // a read of LDS
-                __builtin_amdgcn_sched_group_barrier(0x008, kPer, 0);  // kPer products
+                if constexpr (!kAmong) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x008, kPer, 0);
+                if constexpr (kAmong) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // a read
             }
             // holds the products here: nothing else would keep the compiler from
             // moving them past the barrier, behind the wait that they should fill
@@ -456,6 +466,8 @@ struct Pipe {
                 for (int t = 0; t < 4; ++t) asm volatile("" : "+v"(acc[x][t]));
             __builtin_amdgcn_sched_barrier(0);
         };
+        const std::true_type yes;
+        const std::false_type no;
 #pragma unroll
         for (int x = 0; x < TM; ++x)
 #pragma unroll
@@ -465,20 +477,24 @@ struct Pipe {
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         read(0, 0, 0);
         math.advance();
-        for (int s = 0; s < steps; ++s) {
-            half(0, s);
+        const auto step = [&](auto load_too, int s) {
+            half(no, 0, s);
             // every wave has read stage s and has its part of stage s + 1
-            if (s > 0) wait(s + kStages - 1 < steps);
+            if (s > 0) arrive();
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            if (s + kStages < steps) {
+            if (s + 2 < steps) {
                 math.commit(extra, s + 2);
-                load(s + kStages);
-                if (s + 3 < steps) math.prefetch();
+                if constexpr (!kAmong) load(s + 2);
             }
+            if (s + 3 < steps) math.prefetch();
             __builtin_amdgcn_sched_barrier(0);
-            half(1, s);  // behind the last step: reads that nothing uses
+            half(load_too, 1, s);  // behind the last step: reads that nothing uses
             math.advance();
-        }
+        };
+        int s = 0;
+        if constexpr (kAmong)
+            for (; s + 2 < steps; ++s) step(yes, s);
+        for (; s < steps; ++s) step(no, s);
         // no wave still reads the stages when this one goes on
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     }
@@ -506,7 +522,7 @@ __device__ __forceinline__ void make_tiles(Pi& pipe, uint32_t b, uint32_t all, F
     if (!from(&job)) return;
     start(job);
     pipe.issue(job.steps);
-    pipe.arrive(job.steps);
+    pipe.arrive();
     for (;;) {
         Job next;
         bool more = false;
@@ -519,7 +535,7 @@ __device__ __forceinline__ void make_tiles(Pi& pipe, uint32_t b, uint32_t all, F
         if (more) {
             start(next);
             pipe.issue(next.steps);
-            pipe.arrive(next.steps);
+            pipe.arrive();
         }
         finish(job, acc);
         if (!more) return;
@@ -582,8 +598,6 @@ __device__ __forceinline__ u32x2 pack4(const f32x4& a) {
     return u32x2{pack_bf16_rne(a[0], a[1]), pack_bf16_rne(a[2], a[3])};
 }
 
-// Places [lo, hi) of a tile as rows of x for the operand q: a place without a
-// row reads `other`, any row of the same length, and its results are not used.
 // A tile of rows as a job of make_tiles().
 struct RowJob {
     Tile t;
@@ -600,6 +614,8 @@ __device__ __forceinline__ int find_rows(const Groups& g, uint32_t b, uint32_t n
     return found;
 }
 
+// Places [lo, hi) of a tile as rows of x for the operand q: a place without a
+// row reads `other`, any row of the same length, and its results are not used.
 template <typename S, int B, bool kWhole>
 __device__ __forceinline__ void start_rows(RowOperand<S, B, false, kWhole>& q, const Tile& t, const char* x,
                                            const Rows& rows, const char* other, int64_t bytes) {
@@ -626,18 +642,23 @@ cobalt_status over_tiles(int64_t all, F&& kernel) {
 
 // The tiles of a product are chosen by what they are expected to take: rounds
 // of workgroups over the 256 CUs, times what the workgroups that share a CU
-// work at once, in units of 32 x 256 results. Tiles that fill LDS less let
-// two or three workgroups share a CU, but read more of it per product. With
-// 16384 rows of 8 experts, 7168 x 2048, a unit and step takes (gate_up)
-//   bf16:  256 x 256 0.237 us, 192 x 256 0.238, 64 x 256 0.29, 64 x 128 0.39
-//   4-bit: 192 x 256 0.33 us, 128 x 256 0.38, 64 x 128 0.56 (256 x 256 does
-//          not fit into the registers with the scales: 0.47)
-// Tile by tile, with 256 x 256 | 192 x 256 | 64 x 256 | 64 x 128, in us:
-//   gate_up   16384 rows,   8 experts, 7168 x 2048:  1062 |  963 | 1184 | 1456
-//   its dh    16384 rows,   8 experts, 7168 x 2048:   760 |  644 |  737 |  906
-//   its dh    24576 rows,  64 experts, 2048 x 1024:   208 |  256 |  223 |  260
-//   gate_up    4096 rows, 128 experts, 2048 x 1024:   319 |  299 |  242 |  256
-//   gate_up    1018 rows,  16 experts,  512 x  256:    23 |   19 |   12 |   10
+// take for a step at once. Tiles that fill LDS less let two or three
+// workgroups share a CU, so that one multiplies while another begins or ends a
+// tile, but read more of it per product. Measured in us:
+//                                                  256x256 192x128 64x256 64x128
+//   gate_up, 16384 rows, 8 experts, 7168 x 2048       912     897   1180   1350
+//   gate_up,  6126 rows, 64 experts, 2048 x 1000      211     164    145    158
+//   its dh,  16384 rows, 8 experts, 7168 x 2048       746     559    701    716
+//   its dh,  24576 rows, 64 experts, 2048 x 1024      201     213    215    222
+//   weights, 16384 rows, 8 experts, 7168 x 2048       573       -    666    737
+//   gate_up,  1018 rows, 16 experts, 512 x 256         23      19     12     10
+//                                                  192x256 128x256        64x128
+//   gate_up, the first of these in 4 bits             315     362           447
+//   down, 4096 rows, 8 experts, 2048 x 7168            72      60            69
+// 256 x 256 tiles are left out where both operands lie along k, as they won
+// by 2 % at most there, and 192 x 128 ones where neither does, as a lane's 16
+// bytes do not divide such lines evenly. 4-bit tiles of 256 x 256 do not fit
+// into the registers with their scales: 405 us.
 struct Choice {
     int64_t tiles;
     int per_cu;    // workgroups that fit on a CU
@@ -658,39 +679,44 @@ inline int64_t expected_tiles(const Groups& g, int BM) {
     return (int64_t)std::ceil(std::max(with, M / BM + with / 2));
 }
 
-// What the rows of a product's tiles are: rows in memory, of bf16 or 4-bit
-// values, or columns.
-enum class Along { kRows, kMxRows, kColumns };
+// What lies along k in memory: both operands, of bf16 or 4-bit values, one of
+// them, or neither.
+enum class Along { kBoth, kMxBoth, kOne, kNeither };
 
 // Calls f(shape) with the shape whose count(shape) tiles of so many steps cost
-// least. (Where the rows are k, tiles differ in their steps, and the results
-// take about as long as the products: beginning counts as nothing there.)
+// least. Where the places are k, tiles differ in their steps, and the results
+// take about as long as the products: beginning counts as nothing there.
 template <Along kAlong, typename C, typename F>
 cobalt_status by_shape(int64_t steps, C&& count, F&& f) {
-    constexpr double kBegin = kAlong == Along::kColumns ? 0.0 : 2.0;
+    constexpr double kBegin = kAlong == Along::kNeither ? 0.0 : 2.0;
+    // workgroups on a CU, and what a step of theirs takes
+    struct Cost {
+        int per_cu;
+        double work;
+    };
+    const auto cost = [&](auto shape, Cost c) {
+        const double begin = c.per_cu == 1 ? kBegin * 1.5 : kBegin;
+        return Choice{count(shape), c.per_cu, c.work, begin}.cost(steps);
+    };
     const Shape<2, 2> small;
-    const double a = Choice{count(small), 3, 1.95, kBegin}.cost(steps);
-    if constexpr (kAlong == Along::kMxRows) {
+    const Shape<4, 2> low;
+    const Shape<2, 6> high;
+    const Shape<4, 8> large;
+    const double a = cost(small, {3, 1.95});
+    if constexpr (kAlong == Along::kMxBoth) {
         const Shape<4, 4> middle;
-        const Shape<4, 6> large;
-        const double b = Choice{count(middle), 1, 4.6, kBegin + 1}.cost(steps),
-                     c = Choice{count(large), 1, 6.0, kBegin + 1}.cost(steps);
-        return c <= a && c <= b ? f(large) : b <= a ? f(middle) : f(small);
+        const Shape<4, 6> wide;
+        const double b = cost(middle, {1, 4.6}), c = cost(wide, {1, 6.0});
+        return c <= a && c <= b ? f(wide) : b <= a ? f(middle) : f(small);
     } else {
-        const Shape<4, 2> low;
-        const Shape<4, 8> large;
-        const double b = Choice{count(low), 2, 2.8, kBegin}.cost(steps),
-                     c = Choice{count(large), 1, 8.0, kBegin * 1.5}.cost(steps);
-        const auto others = [&] {
-            return c <= a && c <= b ? f(large) : b <= a ? f(low) : f(small);
-        };
-        if constexpr (kAlong == Along::kColumns) {
-            return others();
-        } else {
-            const Shape<2, 6> high;
-            const double d = Choice{count(high), 2, 3.35, kBegin}.cost(steps);
-            return d < a && d < b && d < c ? f(high) : others();
-        }
+        const double b = cost(low, {2, 2.8});
+        const double c = kAlong != Along::kNeither ? cost(high, {2, 3.35}) : INFINITY;
+        const double d = kAlong != Along::kBoth ? cost(large, {1, 8.0}) : INFINITY;
+        if constexpr (kAlong != Along::kBoth)
+            if (d <= a && d <= b && d <= c) return f(large);
+        if constexpr (kAlong != Along::kNeither)
+            if (c < a && c < b) return f(high);
+        return b <= a ? f(low) : f(small);
     }
 }
 // The same for n columns of the experts' places.
