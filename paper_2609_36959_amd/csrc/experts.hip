@@ -84,13 +84,15 @@ __global__ __launch_bounds__(S::kThreads, 2) void gate_up_gradient_kernel(
 }
 
 // Tiles of all experts' gradients, expert by expert; mt: tiles along m of one.
+// With `parts` > 1 each expert's places are split into that many runs, and
+// result part * E + e is the sum over run `part` of expert e.
 struct GradJob {
     int64_t m0, n0;
-    int e, lo, hi, steps;
+    int to, lo, hi, steps;
 };
 template <typename S, bool kFloat, bool kAdd, bool kGatherA, bool kGatherB>
 __global__ __launch_bounds__(S::kThreads, 2) void weight_gradient_kernel(
-    Groups g, uint32_t b0, uint32_t all, uint32_t mt, const char* a, int64_t na, const char* b,
+    Groups g, uint32_t b0, uint32_t all, uint32_t mt, uint32_t parts, const char* a, int64_t na, const char* b,
     int64_t nb, Rows rows, void* dw) {
     constexpr int kBM = S::kBM, kBN = S::kBN;
     typedef Lds<S, Bf16Math<S>, true> L;
@@ -103,11 +105,15 @@ __global__ __launch_bounds__(S::kThreads, 2) void weight_gradient_kernel(
         pipe, b0 + blockIdx.x, all,
         [&](uint32_t id, GradJob* job) {
             const TileAt at = tile_at(id, (uint32_t)((nb + kBN - 1) / kBN));
-            if (at.m / kBand * kBand >= mt * (uint32_t)g.E) return -1;
-            const int e = (int)(at.m / mt);
-            if (e >= g.E) return 0;
-            const int lo = min(max(g.off[e], 0), g.M), hi = min(max(g.off[e + 1], 0), g.M);
-            *job = {(int64_t)(at.m % mt) * kBM, (int64_t)at.n * kBN, e, lo, hi,
+            const uint32_t of = at.m / mt;  // expert of * parts + part
+            if (at.m / kBand * kBand >= mt * parts * (uint32_t)g.E) return -1;
+            if (of >= parts * (uint32_t)g.E) return 0;
+            const int e = (int)(of / parts), part = (int)(of % parts);
+            int lo = min(max(g.off[e], 0), g.M), hi = min(max(g.off[e + 1], 0), g.M);
+            const int steps = hi > lo ? (hi - lo + 63) / 64 : 0;
+            const int64_t run = (steps + (int)parts - 1) / (int)parts * (int64_t)64;
+            lo = (int)min(lo + part * run, (int64_t)hi), hi = (int)min(lo + run, (int64_t)hi);
+            *job = {(int64_t)(at.m % mt) * kBM, (int64_t)at.n * kBN, part * g.E + e, lo, hi,
                     hi > lo ? (hi - lo + 63) / 64 : 0};
             return 1;
         },
@@ -123,7 +129,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void weight_gradient_kernel(
             store_rows<S>(L::turn(lds), acc, [&](int r, int c, const f32x4 (&v)[2]) {
                 const int64_t m = job.m0 + r, n = job.n0 + c;
                 if (m >= na || n >= nb) return;
-                const int64_t i = ((int64_t)job.e * na + m) * nb + n;
+                const int64_t i = ((int64_t)job.to * na + m) * nb + n;
                 if constexpr (!kFloat) {
                     *(u32x4*)((uint16_t*)dw + i) = pack8(v[0], v[1]);
                 } else {
@@ -133,6 +139,34 @@ __global__ __launch_bounds__(S::kThreads, 2) void weight_gradient_kernel(
                 }
             });
         });
+}
+
+// dw = the sum of `parts` partial gradients of n values each, n % 4 == 0, in
+// their order.
+template <bool kFloat, bool kAdd>
+__global__ __launch_bounds__(256) void add_parts_kernel(const float* from, int parts, int64_t n,
+                                                        void* dw) {
+    const int64_t i = (blockIdx.x * (int64_t)256 + threadIdx.x) * 4;
+    if (i >= n) return;
+    f32x4 v = *(const f32x4*)(from + i);
+    for (int p = 1; p < parts; ++p) v += *(const f32x4*)(from + p * n + i);
+    if constexpr (!kFloat) {
+        *(u32x2*)((uint16_t*)dw + i) = pack4(v);
+    } else {
+        f32x4* to = (f32x4*)((float*)dw + i);
+        *to = kAdd ? *to + v : v;
+    }
+}
+
+// Into how many runs the places of each expert are split for a gradient of
+// na x nb values: 1 unless even the smallest tiles leave places on the CUs, for
+// three workgroups each, that other runs could take with eight steps or more
+// to do. Output projections' gradients, split and not: 16384 rows of 4 experts
+// of 512 x 256 20 and 56 us, 65536 of one of 1024 x 1024 226 and 959.
+int parts_of(int64_t M, int E, int64_t na, int64_t nb) {
+    typedef Shape<2, 2> S;
+    const int64_t all = E * tiles(na, S::kBM) * tiles(nb, S::kBN);
+    return (int)std::max<int64_t>(1, std::min<int64_t>(3 * 256 / all, M / E / 64 / 8));
 }
 
 }  // namespace
@@ -193,27 +227,41 @@ cobalt_status launch_gate_up_gradient(const Groups& g, const void* dgate_up, int
 cobalt_status launch_weight_gradient(const Groups& g, const void* a, int64_t na, bool a_rows,
                                      const void* b, int64_t nb, Rows rows, void* dw,
                                      bool f32, bool add, void* ws, hipStream_t s) {
-    const auto run = [&](auto shape, auto in_float, auto in_add, auto ga, auto gb) {
+    const auto run = [&](auto shape, auto in_float, auto in_add, auto ga, auto gb, int parts,
+                         void* to) {
         typedef decltype(shape) S;
         const int64_t mt = tiles(na, S::kBM);
         return over_tiles<S::kStays>(
-            tile_grid(mt * g.E, tiles(nb, S::kBN)), [&](uint32_t b0, unsigned n, uint32_t all) {
+            tile_grid(mt * parts * g.E, tiles(nb, S::kBN)),
+            [&](uint32_t b0, unsigned n, uint32_t all) {
                 weight_gradient_kernel<S, in_float(), in_add(), ga(), gb()>
-                    <<<n, S::kThreads, 0, s>>>(g, b0, all, (uint32_t)mt, (const char*)a, na,
-                                               (const char*)b, nb, rows, dw);
+                    <<<n, S::kThreads, 0, s>>>(g, b0, all, (uint32_t)mt, (uint32_t)parts,
+                                               (const char*)a, na, (const char*)b, nb, rows, to);
             });
     };
     // rows without an index are the places; one operand at most has one
     const std::true_type yes;
     const std::false_type no;
-    const auto gather = [&](auto shape, auto in_float, auto in_add) {
-        if (!rows.idx) return run(shape, in_float, in_add, no, no);
-        return a_rows ? run(shape, in_float, in_add, yes, no)
-                      : run(shape, in_float, in_add, no, yes);
+    const auto gather = [&](auto shape, auto in_float, auto in_add, int parts, void* to) {
+        if (!rows.idx) return run(shape, in_float, in_add, no, no, parts, to);
+        return a_rows ? run(shape, in_float, in_add, yes, no, parts, to)
+                      : run(shape, in_float, in_add, no, yes, parts, to);
     };
+    if (const int parts = parts_of(g.M, g.E, na, nb); parts > 1) {
+        if (cobalt_status st = gather(Shape<2, 2>(), yes, no, parts, ws)) return st;
+        return by_bool(f32, [&](auto in_float) {
+            return by_bool(f32 && add, [&](auto in_add) {
+                const int64_t n = g.E * na * nb;
+                add_parts_kernel<in_float(), in_add()>
+                    <<<(unsigned)tiles(n, 1024), 256, 0, s>>>((const float*)ws, parts, n, dw);
+                COBALT_LAUNCH_CHECK();
+                return COBALT_OK;
+            });
+        });
+    }
     const auto by_type = [&](auto shape) {
-        if (!f32) return gather(shape, no, no);
-        return add ? gather(shape, yes, yes) : gather(shape, yes, no);
+        if (!f32) return gather(shape, no, no, 1, dw);
+        return add ? gather(shape, yes, yes, 1, dw) : gather(shape, yes, no, 1, dw);
     };
     return by_shape<Along::kNeither>(
         1,
@@ -224,6 +272,13 @@ cobalt_status launch_weight_gradient(const Groups& g, const void* a, int64_t na,
         by_type);
 }
 
-size_t expert_backward_workspace_bytes(int64_t, int, int64_t, int64_t) { return 256; }
+size_t expert_backward_workspace_bytes(int64_t M, int E, int64_t d, int64_t f) {
+    size_t most = 256;
+    for (const int64_t width : {f, 2 * f}) {  // of dw_down and dw_in
+        const int parts = width == f ? parts_of(M, E, d, f) : parts_of(M, E, width, d);
+        if (parts > 1) most = std::max(most, (size_t)(parts * E * d * width * 4));
+    }
+    return (most + 255) / 256 * 256;
+}
 
 }  // namespace cobalt

@@ -630,7 +630,7 @@ __device__ __forceinline__ void start_rows(RowOperand<S, B, false, kWhole>& q, c
 template <bool kStays, typename F>
 cobalt_status over_tiles(int64_t all, F&& kernel) {
     constexpr int64_t kCus = 256;
-    const int64_t most = kStays ? kCus : kMaxLaunchItems / 512 / 256 * 256;
+    const int64_t most = kStays ? kCus : std::max<int64_t>(1, max_launch_items() / 512);
     if (all > INT32_MAX) return COBALT_EUNSUPPORTED;
     for (int64_t b0 = 0; b0 < all; b0 += most) {
         kernel((uint32_t)b0, (unsigned)std::min(all - b0, most), (uint32_t)all);
@@ -650,6 +650,7 @@ cobalt_status over_tiles(int64_t all, F&& kernel) {
 //   gate_up,  6126 rows, 64 experts, 2048 x 1000      211     164    145    158
 //   its dh,  16384 rows, 8 experts, 7168 x 2048       746     559    701    716
 //   its dh,  24576 rows, 64 experts, 2048 x 1024      201     213    215    222
+//   its dx,  16384 rows, 8 experts, 7168 x 2048       994     942   1198   1301
 //   weights, 16384 rows, 8 experts, 7168 x 2048       573       -    666    737
 //   gate_up,  1018 rows, 16 experts, 512 x 256         23      19     12     10
 //                                                  192x256 128x256        64x128
@@ -711,7 +712,9 @@ cobalt_status by_shape(int64_t steps, C&& count, F&& f) {
     } else {
         const double b = cost(low, {2, 2.8});
         const double c = kAlong != Along::kNeither ? cost(high, {2, 3.35}) : INFINITY;
-        const double d = kAlong != Along::kBoth ? cost(large, {1, 8.0}) : INFINITY;
+        const double d = kAlong == Along::kOne       ? cost(large, {1, 8.6})
+                         : kAlong == Along::kNeither ? cost(large, {1, 8.0})
+                                                     : INFINITY;
         if constexpr (kAlong != Along::kBoth)
             if (d <= a && d <= b && d <= c) return f(large);
         if constexpr (kAlong != Along::kNeither)
