@@ -1,0 +1,166 @@
+"""A step of a mixture-of-experts layer on the GPU: a routing step's dispatched
+rows through the experts' gated feed-forward, the combine, and the gradients of
+all of it; and the same layer serving tokens with 4-bit experts.
+
+    python -m paper_2609_36959_amd.experts [--workload tiny] [--width 256] [--steps 5]
+
+runs both and prints their times."""
+from __future__ import annotations
+
+import argparse
+from typing import Optional
+
+import torch
+
+from . import binding as B
+from . import pipeline as PL
+from . import workload as W
+
+BF16, I32, U8 = torch.bfloat16, torch.int32, torch.uint8
+
+
+def draw_weights(E: int, d: int, f: int, seed: int, device="cuda"):
+    """w_in [E, 2f, d] (gate rows, then up rows) and w_down [E, d, f], random
+    values that keep the rows' size."""
+    gen = torch.Generator(device=device)
+    gen.manual_seed(seed)
+    return tuple((torch.randn(shape, generator=gen, device=device) * shape[-1] ** -0.5).to(BF16)
+                 for shape in ((E, 2 * f, d), (E, d, f)))
+
+
+class ExpertStep(PL.RoutingStep):
+    """A routing step whose experts are there: expert_out, drawn by a plain
+    routing step, is computed from the packed rows. All ranks are this GPU's
+    memory, and replicas of an expert share its weights, so places are grouped
+    by expert whatever rank they were sent to."""
+
+    def __init__(self, w: W.Workload, seed: int, f: int, act: int = B.ACT_SILU, device="cuda",
+                 **routing):
+        super().__init__(w, seed, device=device, expert_out="roundtrip", **routing)
+        dev, M, d = self.device, w.T * w.K, w.d
+        self.f, self.act = f, act
+        self.w_in, self.w_down = draw_weights(w.E, d, f, seed, device)
+        self.rows = torch.empty(M, dtype=I32, device=dev)
+        self.expert_offsets = torch.empty(w.E + 1, dtype=I32, device=dev)
+        self.group_workspace = B.expert_group_workspace_for(w.T, w.K, w.E, device=dev)
+        self.h = torch.empty(M, f, dtype=BF16, device=dev)
+        self.gate_up = torch.empty(M, 2 * f, dtype=BF16, device=dev)
+        self.eo = torch.empty(M, d, dtype=BF16, device=dev)
+
+    def forward(self, mode=0, stream=None):
+        """x -> y: dispatch, the experts' rows, combine."""
+        self.stats(stream)
+        self.assign(mode, stream)
+        self.pack(stream)
+        B.cobalt_expert_group(self.topk, self.pos, self.w.E, self.rows, self.expert_offsets,
+                              self.group_workspace, stream=stream)
+        B.cobalt_expert_gate_up(self.packed, self.rows, self.expert_offsets, self.w_in, self.h,
+                                self.gate_up, act=self.act, stream=stream)
+        B.cobalt_expert_down(self.h, self.expert_offsets, self.w_down, self.rows, self.eo,
+                             stream=stream)
+        self.combine(stream=stream)
+
+    def backward(self, dy: torch.Tensor, flags: int = 0, stream=None):
+        """dy -> dx, dgates and the weights' gradients, of the last forward().
+        flags: B.GRAD_FLOAT, B.GRAD_ADD (with zeroed dw_in and dw_down before
+        the first step). Buffers are allocated on first use."""
+        w, M = self.w, self.w.T * self.w.K
+        if getattr(self, "deo", None) is None:
+            like = torch.empty_like
+            self.deo, self.dpacked = like(self.eo), like(self.packed)
+            self.dgates, self.dx = like(self.gates), like(self.x)
+            kind = torch.float32 if flags & B.GRAD_FLOAT else BF16
+            self.dw_in = torch.zeros_like(self.w_in, dtype=kind)
+            self.dw_down = torch.zeros_like(self.w_down, dtype=kind)
+            self.ones = torch.ones_like(self.gates)
+            self.backward_workspace = B.expert_backward_workspace_for(M, w.E, w.d, self.f,
+                                                                      device=self.device)
+        B.cobalt_combine_backward(dy, self.eo, self.pos, self.gates, self.deo, self.dgates,
+                                  stream=stream)
+        # the activation's gradient takes its input's place
+        B.cobalt_expert_down_backward(self.deo, self.rows, self.expert_offsets, self.w_down,
+                                      self.gate_up, self.h, self.gate_up, self.dw_down,
+                                      self.backward_workspace, act=self.act, flags=flags,
+                                      stream=stream)
+        B.cobalt_expert_gate_up_backward(self.gate_up, self.packed, self.rows,
+                                         self.expert_offsets, self.w_in, self.dpacked, self.dw_in,
+                                         self.backward_workspace, flags=flags, stream=stream)
+        # the dispatch copies a token's row to each of its pairs: its gradient
+        # is their sum
+        B.cobalt_combine(self.dpacked, self.pos, self.ones, self.dx, stream=stream)
+
+
+class MxExperts:
+    """4-bit experts that serve up to T tokens of K pairs each: the weights are
+    quantised once, and a token's row once for all its pairs."""
+
+    def __init__(self, w_in: torch.Tensor, w_down: torch.Tensor, T: int, K: int,
+                 act: int = B.ACT_SILU):
+        (E, d, f), dev = w_down.shape, w_in.device
+        self.E, self.d, self.f, self.K, self.act = E, d, f, K, act
+        self.w_in, self.w_down = self.codes(E, 2 * f, d, dev), self.codes(E, d, f, dev)
+        B.cobalt_mx_quantize(w_in, *self.w_in)
+        B.cobalt_mx_quantize(w_down, *self.w_down)
+        M = T * K
+        self.rows, self.tokens = torch.empty(2, M, dtype=I32, device=dev)
+        self.expert_offsets = torch.empty(E + 1, dtype=I32, device=dev)
+        self.workspace = B.expert_group_workspace_for(T, K, E, device=dev)
+        self.x, self.hq = self.codes(T, d, dev), self.codes(M, f, dev)
+        self.h = torch.zeros(M, f, dtype=BF16, device=dev)
+        self.out = torch.empty(M, d, dtype=BF16, device=dev)
+        self.pos = torch.arange(M, dtype=I32, device=dev).view(T, K)
+
+    @staticmethod
+    def codes(*shape):
+        *lead, n, device = shape
+        return tuple(torch.empty(*lead, n // k, dtype=U8, device=device) for k in (2, 32))
+
+    def run(self, x: torch.Tensor, topk: torch.Tensor, gates: torch.Tensor, y: torch.Tensor,
+            pos: Optional[torch.Tensor] = None, stream=None):
+        """y[t] = the gated sum of the experts' outputs for x[t]. pos: each
+        pair's number t * K + k, or -1 for a pair that was dropped (its expert
+        is outside [0, E)); None if none was."""
+        T, K = topk.shape
+        M = T * K
+        rows, tokens, h, out = self.rows[:M], self.tokens[:M], self.h[:M], self.out[:M]
+        xq, hq = [t[:T] for t in self.x], [t[:M] for t in self.hq]
+        B.cobalt_expert_group(topk, None, self.E, rows, self.expert_offsets, self.workspace,
+                              tokens=tokens, stream=stream)
+        B.cobalt_mx_quantize(x, *xq, stream=stream)
+        B.cobalt_mx_gate_up(*xq, tokens, self.expert_offsets, *self.w_in, h, act=self.act,
+                            stream=stream)
+        B.cobalt_mx_quantize(h, *hq, stream=stream)
+        B.cobalt_mx_down(*hq, self.expert_offsets, *self.w_down, rows, out, stream=stream)
+        B.cobalt_combine(out, self.pos[:T] if pos is None else pos, gates, y, stream=stream)
+
+
+def main(argv=None):
+    a = argparse.ArgumentParser(description=__doc__,
+                                formatter_class=argparse.RawDescriptionHelpFormatter)
+    a.add_argument("--workload", default="tiny", choices=sorted(W.WORKLOADS))
+    a.add_argument("--width", type=int, default=256, help="columns of an expert's hidden rows")
+    a.add_argument("--steps", type=int, default=5)
+    a = a.parse_args(argv)
+    w = W.WORKLOADS[a.workload]
+    step = ExpertStep(w, w.seed, a.width)
+    serve = MxExperts(step.w_in, step.w_down, w.T, w.K)
+    dy, y = torch.randn_like(step.y), torch.empty_like(step.y)
+    runs = {"training step": lambda: (step.forward(), step.backward(dy)),
+            "4-bit serving": lambda: serve.run(step.x, step.topk, step.gates, y)}
+    for what, run in runs.items():
+        run()
+        begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        begin.record()
+        for _ in range(a.steps):
+            run()
+        end.record()
+        end.synchronize()
+        ms = begin.elapsed_time(end) / a.steps
+        print(f"{what}: {ms:.3f} ms for {w.T} tokens, {w.E} experts of {w.d} x {a.width}")
+    far = float((y.float() - step.y.float()).norm() / step.y.float().norm())
+    print(f"4-bit outputs differ from bf16 ones by {far:.3f} of their norm")
+    step.close()
+
+
+if __name__ == "__main__":
+    main()
