@@ -8,6 +8,10 @@
 // eight waves are KS parts of k by 8 / KS groups of 16 rows, KS the largest
 // that leaves a wave kLeast steps; their sums meet in LDS and are added in
 // the order of the parts.
+//
+// Bound by memory: one token's 8 of 64 experts of 4096 x 1024 take 28 us for
+// gate_up, 134 MB at 4.8 TB/s, and 17 us for down, 67 MB, where most of the
+// time is the launch's own beginning and end.
 #pragma once
 
 #include "forward.hpp"
@@ -148,16 +152,25 @@ cobalt_status by_parts(int64_t bytes, F&& f) {
     return f(std::integral_constant<int, 1>());
 }
 
-// Whether products with n weight rows stream the weights: while tiles of 64 x
-// 128 would leave CUs without work, whose loads of a step then wait for the
-// step before. With experts of 4096 x 1024 out of memory, in us, streamed | in
-// tiles:
-//   places      1           4           8          16          64
-//   gate_up  13 |  35    16 |  45    30 |  57    52 |  60    99 |  86
-//   down      7 |  11    10 |  13    18 |  18    31 |  22    63 |  50
+// Whether products with n weight rows of `bytes` bytes stream the weights: while
+// tiles of 64 x 128 would leave CUs without work, and an expert has about 16
+// places at most: or a half more, if its weights, taken once for every 16
+// places, take less than a tile's steps one after another. Streamed | in tiles,
+// in us, weights out of memory:
+//   experts of 4096 x 1024, places  1           4           8          16
+//     gate_up                   13 |  35    16 |  45    30 |  57    52 |  60
+//     down                       7 |  11    10 |  13    18 |  18    31 |  22
+//   8 experts of 7168 x 2048        8          32          64         128
+//     gate_up                   65 |  97    94 | 105   102 | 105   145 | 106
+//   4 experts of 2048 x 512        16          64         128         256
+//     gate_up                   10 |  20    11 |  21    19 |  21    27 |  20
+//     down                       7 |   8     8 |   8    13 |   8    19 |   8
 // (4-bit products take as long in tiles from one place on.)
-inline bool few_rows(const Groups& g, int64_t n) {
-    return expected_tiles(g, 64) * tiles(n, 128) <= 256;
+inline bool few_rows(const Groups& g, int64_t n, int64_t bytes) {
+    if (expected_tiles(g, 64) * tiles(n, 128) > 256) return false;
+    const int64_t once = expected_tiles(g, INT32_MAX), all = expected_tiles(g, kFewPlaces);
+    return all <= once || (2 * all <= 3 * once && (double)all * n * bytes / 5e12 <
+                                                      tiles(bytes, kStepBytes) * 0.6e-6);
 }
 
 // Workgroups for n columns.
@@ -170,7 +183,7 @@ cobalt_status gate_up(const Groups& g, const Side& x, Rows rows, const Side& w, 
                       void* h, void* gu, hipStream_t s) {
     return by_act(act, [&](auto a) {
         if constexpr (!Side::kScaled)
-            if (few_rows(g, f * 2))
+            if (few_rows(g, f * 2, w.bytes))
                 return by_parts(w.bytes, [&](auto ks) {
                     return over_tiles<false>(
                         few_grid(g, f, ks()), [&](uint32_t b0, unsigned n, uint32_t) {
@@ -194,7 +207,7 @@ template <typename Side>
 cobalt_status down(const Groups& g, const Side& h, const Side& w, int64_t d, Rows rows, void* out,
                    hipStream_t s) {
     if constexpr (!Side::kScaled)
-        if (few_rows(g, d))
+        if (few_rows(g, d, w.bytes))
             return by_parts(w.bytes, [&](auto ks) {
                 return over_tiles<false>(
                     few_grid(g, d, ks()), [&](uint32_t b0, unsigned n, uint32_t) {

@@ -15,6 +15,9 @@
 // to each. Up to kSelfPairs pairs each workgroup counts all pairs itself, which
 // costs less than a launch; beyond, count_kernel first writes the counts of
 // every tile, [tiles][E], and each workgroup sums them.
+//
+// 16384 pairs of 8 experts take 13 us, 6126 of 64 8 us, 8 of 64 5 us; their
+// bytes are nothing, the steps' latencies one after another are all of it.
 #include <algorithm>
 
 #include "internal.hpp"

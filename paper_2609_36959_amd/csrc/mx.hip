@@ -1,9 +1,15 @@
 // Microscaled 4-bit rows: quantisation, and the experts' products on them.
+//
+// The products are the bf16 ones' kernels on 4-bit operands (two codes a byte,
+// 256 values of k a step) with the matrix cores' block scales. 16384 rows of 8
+// experts of 7168 x 2048: gate_up 315 us, 3.05 PFLOP/s, down 200 us, 2.4
+// PFLOP/s; their matrix instructions are busy a third of the time, and waves
+// wait for the loads of a step, which arrive at 64 bytes a cycle and CU. One
+// token's 8 experts of 4096 x 1024: 16 and 7 us, 36 and 18 MB.
 #include "few.hpp"
 
 namespace cobalt {
 namespace {
-
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
@@ -11,7 +17,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 // scales pass in whole lines. Rounding and division by the scale are one
 // conversion per two values (to nearest, ties to the even code, larger
 // magnitudes to 6; of the scale only the exponent counts, and exponent 0 is
-// 2^-127). Bound by memory: 65536 x 7168 in QQ us, QQ TB/s.
+// 2^-127). Bound by memory: 65536 x 7168 in 190 us, 6.3 TB/s.
 __global__ __launch_bounds__(256) void quantize_kernel(const u32x4* __restrict__ x, int64_t eights,
                                                        uint32_t* __restrict__ codes,
                                                        uint8_t* __restrict__ scales) {
@@ -37,7 +43,7 @@ __global__ __launch_bounds__(256) void quantize_kernel(const u32x4* __restrict__
     if (i % 4 == 0) scales[i / 4] = (uint8_t)ex;
 }
 
-// Eight values a lane, exact in bf16. 65536 x 7168 in QQ us, QQ TB/s.
+// Eight values a lane, exact in bf16. 65536 x 7168 in 160 us, 7.4 TB/s.
 __global__ __launch_bounds__(256) void dequantize_kernel(const uint32_t* __restrict__ codes,
                                                          const uint8_t* __restrict__ scales,
                                                          int64_t eights, u32x4* __restrict__ y) {
