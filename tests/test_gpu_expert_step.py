@@ -108,6 +108,36 @@ def test_serving_in_four_bits(step):
         assert np.array_equal(PL.bf16_bits(y), want)
 
 
+def test_captured_in_a_graph(step):
+    """A captured step gives the eager step's outputs on every replay, with
+    eager work between the replays, and follows its inputs' values."""
+    dy = C.dev(C.bf16(np.random.default_rng(6), step.w.T, step.w.d))
+    serve = M.MxExperts(step.w_in, step.w_down, step.w.T, step.w.K)
+    y4 = torch.empty_like(step.y)
+
+    def run():
+        step.forward()
+        step.backward(dy)
+        serve.run(step.x, step.topk, step.gates, y4)
+        return [step.y, step.dx, step.dgates, step.dw_in, step.dw_down, y4]
+
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = run()
+    for i in range(4):
+        step.x.mul_(0.5 if i % 2 else 2.0)
+        want = [t.clone() for t in run()]
+        for t in outs:
+            t.fill_(7.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for p, q in zip(want, outs):
+            assert torch.equal(p, q)
+
+
 def test_command(capsys):
     M.main(["--workload", "tiny", "--width", "64", "--steps", "2"])
     said = capsys.readouterr().out
