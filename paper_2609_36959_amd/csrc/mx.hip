@@ -3,9 +3,10 @@
 // The products are the bf16 ones' kernels on 4-bit operands (two codes a byte,
 // 256 values of k a step) with the matrix cores' block scales. 16384 rows of 8
 // experts of 7168 x 2048: gate_up 315 us, 3.05 PFLOP/s, down 200 us, 2.4
-// PFLOP/s; their matrix instructions are busy a third of the time, and waves
-// wait for the loads of a step, which arrive at 64 bytes a cycle and CU. One
-// token's 8 experts of 4096 x 1024: 16 and 7 us, 36 and 18 MB.
+// PFLOP/s. Bound by how far the parts of a step overlap: 192 x 256 tiles have
+// 1536 cycles of matrix instructions, 1280 of LDS reads and 990 of loads into
+// LDS, and take about 3800. One token's 8 experts of 4096 x 1024: 16 and 7 us,
+// 36 and 18 MB.
 #include "few.hpp"
 
 namespace cobalt {
