@@ -111,14 +111,9 @@ extern "C" cobalt_status cobalt_expert_down_backward(
     if (dw_down && (!aligned(dw_down, 16) || (M > 0 && !rows_ok(h)))) return COBALT_EINVAL;
     const Groups g{off, E, (int32_t)M};
     const Rows at{rows, out_rows};
-    const hipStream_t s = (hipStream_t)stream;
-    if (dw_down)
-        if (cobalt_status st = launch_weight_gradient(g, dout, d, true, h, f, at, dw_down,
-                                                      flags & COBALT_GRAD_FLOAT,
-                                                      flags & COBALT_GRAD_ADD, ws, s))
-            return st;
-    if (!dgate_up || M == 0) return COBALT_OK;
-    return launch_down_gradient(g, dout, at, d, f, w_down, gate_up, (Act)act, dgate_up, s);
+    return launch_down_backward(g, dout, at, d, f, w_down, gate_up, h, (Act)act, dgate_up, dw_down,
+                                flags & COBALT_GRAD_FLOAT, flags & COBALT_GRAD_ADD, ws,
+                                (hipStream_t)stream);
 }
 
 extern "C" cobalt_status cobalt_expert_gate_up_backward(
@@ -134,14 +129,9 @@ extern "C" cobalt_status cobalt_expert_gate_up_backward(
         return COBALT_EINVAL;
     const Groups g{off, E, (int32_t)M};
     const Rows at{rows, x_rows};
-    const hipStream_t s = (hipStream_t)stream;
-    if (dw_in)
-        if (cobalt_status st = launch_weight_gradient(g, dgate_up, 2 * f, false, x, d, at,
-                                                      dw_in, flags & COBALT_GRAD_FLOAT,
-                                                      flags & COBALT_GRAD_ADD, ws, s))
-            return st;
-    if (!dx || M == 0 || x_rows == 0) return COBALT_OK;
-    return launch_gate_up_gradient(g, dgate_up, d, f, w_in, at, dx, s);
+    return launch_gate_up_backward(g, dgate_up, x, at, d, f, w_in, dx, dw_in,
+                                   flags & COBALT_GRAD_FLOAT, flags & COBALT_GRAD_ADD, ws,
+                                   (hipStream_t)stream);
 }
 
 static bool mx_sizes_ok(int64_t R, int64_t n) { return R >= 0 && n >= 32 && n % 32 == 0; }

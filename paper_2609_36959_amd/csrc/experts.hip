@@ -20,16 +20,17 @@ using TurnedPipe = Pipe<S, RowOperand<S, S::kBM, false, kWhole>,
 
 // dh = w^T dout, and through the product and the activation.
 template <typename S, Act A, bool kWhole>
-__global__ __launch_bounds__(S::kThreads, 2) void down_gradient_kernel(
-    Groups g, uint32_t b0, uint32_t all, const char* dout, Rows rows, int64_t d, int64_t f,
-    const char* w, const uint16_t* gu, uint16_t* dgu) {
+__device__ __forceinline__ void down_gradient_tiles(char* lds, const Groups& g, uint32_t b0,
+                                                    uint32_t all, const char* dout,
+                                                    const Rows& rows, int64_t d, int64_t f,
+                                                    const char* w, const uint16_t* gu,
+                                                    uint16_t* dgu) {
     constexpr int kBN = S::kBN;
     typedef Lds<S, Bf16Math<S>, true> L;
-    __shared__ __attribute__((aligned(1024))) char lds[L::kBytes];
     TurnedPipe<S, kWhole> pipe;
     pipe.lds = lds;
     make_tiles<S, RowJob>(
-        pipe, b0 + blockIdx.x, all,
+        pipe, b0, all,
         [&](uint32_t b, RowJob* job) {
             job->steps = (int)((d * 2 + kStepBytes - 1) / kStepBytes);
             return find_rows<S>(g, b, (uint32_t)((f + kBN - 1) / kBN), kBN, job);
@@ -63,16 +64,16 @@ __global__ __launch_bounds__(S::kThreads, 2) void down_gradient_kernel(
 
 // dx = w^T (dgate, dup).
 template <typename S, bool kWhole>
-__global__ __launch_bounds__(S::kThreads, 2) void gate_up_gradient_kernel(
-    Groups g, uint32_t b0, uint32_t all, const char* dgu, int64_t d, int64_t f, const char* w,
-    Rows rows, uint16_t* dx) {
+__device__ __forceinline__ void gate_up_gradient_tiles(char* lds, const Groups& g, uint32_t b0,
+                                                       uint32_t all, const char* dgu, int64_t d,
+                                                       int64_t f, const char* w, const Rows& rows,
+                                                       uint16_t* dx) {
     constexpr int kBN = S::kBN;
     typedef Lds<S, Bf16Math<S>, true> L;
-    __shared__ __attribute__((aligned(1024))) char lds[L::kBytes];
     TurnedPipe<S, kWhole> pipe;
     pipe.lds = lds;
     make_tiles<S, RowJob>(
-        pipe, b0 + blockIdx.x, all,
+        pipe, b0, all,
         [&](uint32_t b, RowJob* job) {
             job->steps = (int)((f * 4 + kStepBytes - 1) / kStepBytes);
             return find_rows<S>(g, b, (uint32_t)((d + kBN - 1) / kBN), kBN, job);
@@ -100,18 +101,18 @@ struct GradJob {
     int to, lo, hi, steps;
 };
 template <typename S, bool kFloat, bool kAdd, bool kGatherA, bool kGatherB>
-__global__ __launch_bounds__(S::kThreads, 2) void weight_gradient_kernel(
-    Groups g, uint32_t b0, uint32_t all, uint32_t mt, uint32_t parts, const char* a, int64_t na, const char* b,
-    int64_t nb, Rows rows, void* dw) {
+__device__ __forceinline__ void weight_gradient_tiles(char* lds, const Groups& g, uint32_t b0,
+                                                      uint32_t all, uint32_t mt, uint32_t parts,
+                                                      const char* a, int64_t na, const char* b,
+                                                      int64_t nb, const Rows& rows, void* dw) {
     constexpr int kBM = S::kBM, kBN = S::kBN;
     typedef Lds<S, Bf16Math<S>, true> L;
-    __shared__ __attribute__((aligned(1024))) char lds[L::kBytes];
     Pipe<S, ColumnOperand<S, kBM, false, kGatherA>, ColumnOperand<S, kBN, false, kGatherB>,
          Bf16Math<S>>
         pipe;
     pipe.lds = lds;
     make_tiles<S, GradJob>(
-        pipe, b0 + blockIdx.x, all,
+        pipe, b0, all,
         [&](uint32_t id, GradJob* job) {
             const TileAt at = tile_at(id, (uint32_t)((nb + kBN - 1) / kBN));
             const uint32_t of = at.m / mt;  // expert of * parts + part
@@ -150,6 +151,62 @@ __global__ __launch_bounds__(S::kThreads, 2) void weight_gradient_kernel(
         });
 }
 
+template <typename S>
+using GradLds = Lds<S, Bf16Math<S>, true>;
+
+template <typename S, Act A, bool kWhole>
+__global__ __launch_bounds__(S::kThreads, 2) void down_gradient_kernel(
+    Groups g, uint32_t b0, uint32_t all, const char* dout, Rows rows, int64_t d, int64_t f,
+    const char* w, const uint16_t* gu, uint16_t* dgu) {
+    __shared__ __attribute__((aligned(1024))) char lds[GradLds<S>::kBytes];
+    down_gradient_tiles<S, A, kWhole>(lds, g, b0 + blockIdx.x, all, dout, rows, d, f, w, gu, dgu);
+}
+
+template <typename S, bool kWhole>
+__global__ __launch_bounds__(S::kThreads, 2) void gate_up_gradient_kernel(
+    Groups g, uint32_t b0, uint32_t all, const char* dgu, int64_t d, int64_t f, const char* w,
+    Rows rows, uint16_t* dx) {
+    __shared__ __attribute__((aligned(1024))) char lds[GradLds<S>::kBytes];
+    gate_up_gradient_tiles<S, kWhole>(lds, g, b0 + blockIdx.x, all, dgu, d, f, w, rows, dx);
+}
+
+template <typename S, bool kFloat, bool kAdd, bool kGatherA, bool kGatherB>
+__global__ __launch_bounds__(S::kThreads, 2) void weight_gradient_kernel(
+    Groups g, uint32_t b0, uint32_t all, uint32_t mt, uint32_t parts, const char* a, int64_t na,
+    const char* b, int64_t nb, Rows rows, void* dw) {
+    __shared__ __attribute__((aligned(1024))) char lds[GradLds<S>::kBytes];
+    weight_gradient_tiles<S, kFloat, kAdd, kGatherA, kGatherB>(lds, g, b0 + blockIdx.x, all, mt,
+                                                               parts, a, na, b, nb, rows, dw);
+}
+
+// The rows' gradients and the weights' of a call in one launch, workgroups
+// [0, all) and [all, all + all_w): neither reads what the other writes. For
+// small calls, whose launches leave CUs idle one after the other (together()).
+typedef Shape<2, 2> Small;
+template <Act A, bool kWhole, bool kFloat, bool kAdd, bool kGather>
+__global__ __launch_bounds__(Small::kThreads, 2) void down_backward_kernel(
+    Groups g, uint32_t all, uint32_t all_w, uint32_t mt, const char* dout, Rows rows, int64_t d,
+    int64_t f, const char* w, const uint16_t* gu, uint16_t* dgu, const char* h, void* dw) {
+    __shared__ __attribute__((aligned(1024))) char lds[GradLds<Small>::kBytes];
+    if (blockIdx.x < all)
+        down_gradient_tiles<Small, A, kWhole>(lds, g, blockIdx.x, all, dout, rows, d, f, w, gu,
+                                              dgu);
+    else
+        weight_gradient_tiles<Small, kFloat, kAdd, kGather, false>(
+            lds, g, blockIdx.x - all, all_w, mt, 1, dout, d, h, f, rows, dw);
+}
+template <bool kWhole, bool kFloat, bool kAdd, bool kGather>
+__global__ __launch_bounds__(Small::kThreads, 2) void gate_up_backward_kernel(
+    Groups g, uint32_t all, uint32_t all_w, uint32_t mt, const char* dgu, int64_t d, int64_t f,
+    const char* w, Rows rows, uint16_t* dx, const char* x, void* dw) {
+    __shared__ __attribute__((aligned(1024))) char lds[GradLds<Small>::kBytes];
+    if (blockIdx.x < all)
+        gate_up_gradient_tiles<Small, kWhole>(lds, g, blockIdx.x, all, dgu, d, f, w, rows, dx);
+    else
+        weight_gradient_tiles<Small, kFloat, kAdd, false, kGather>(
+            lds, g, blockIdx.x - all, all_w, mt, 1, dgu, 2 * f, x, d, rows, dw);
+}
+
 // dw = the sum of `parts` partial gradients of n values each, n % 4 == 0, in
 // their order.
 template <bool kFloat, bool kAdd>
@@ -173,9 +230,39 @@ __global__ __launch_bounds__(256) void add_parts_kernel(const float* from, int p
 // to do. Output projections' gradients, split and not: 16384 rows of 4 experts
 // of 512 x 256 20 and 56 us, 65536 of one of 1024 x 1024 226 and 959.
 int parts_of(int64_t M, int E, int64_t na, int64_t nb) {
-    typedef Shape<2, 2> S;
-    const int64_t all = E * tiles(na, S::kBM) * tiles(nb, S::kBN);
+    const int64_t all = E * tiles(na, Small::kBM) * tiles(nb, Small::kBN);
     return (int)std::max<int64_t>(1, std::min<int64_t>(3 * 256 / all, M / E / 64 / 8));
+}
+
+// The launch of a call's gradients of rows, of n columns, and of na x nb weights
+// in one kernel, if all their tiles are expected to be on the CUs at once.
+struct Both {
+    uint32_t all = 0, all_w = 0, mt = 0;
+    bool ok = false;
+};
+Both together(const Groups& g, int64_t n, int64_t na, int64_t nb) {
+    constexpr int kBM = Small::kBM, kBN = Small::kBN;
+    Both b;
+    if (expected_tiles(g, kBM) * tiles(n, kBN) + g.E * tiles(na, kBM) * tiles(nb, kBN) > 3 * 256 ||
+        parts_of(g.M, g.E, na, nb) > 1)
+        return b;
+    const int64_t all = tile_grid(most_tiles(g.M, g.E, kBM), tiles(n, kBN)),
+                  all_w = tile_grid(tiles(na, kBM) * g.E, tiles(nb, kBN));
+    if ((all + all_w) * Small::kThreads > max_launch_items()) return b;
+    return {(uint32_t)all, (uint32_t)all_w, (uint32_t)tiles(na, kBM), true};
+}
+
+// Calls f(in_float, in_add, gathers).
+template <typename F>
+cobalt_status by_result(bool f32, bool add, bool gathers, F&& f) {
+    return by_bool(f32, [&](auto in_float) {
+        return by_bool(gathers, [&](auto of) {
+            if constexpr (in_float())
+                return by_bool(add, [&](auto in_add) { return f(in_float, in_add, of); });
+            else
+                return f(in_float, in_float, of);
+        });
+    });
 }
 
 }  // namespace
@@ -198,7 +285,7 @@ cobalt_status launch_down(const Groups& g, const void* h, int64_t d, int64_t f,
     });
 }
 
-cobalt_status launch_down_gradient(const Groups& g, const void* dout, Rows rows, int64_t d,
+static cobalt_status launch_down_gradient(const Groups& g, const void* dout, Rows rows, int64_t d,
                                    int64_t f, const void* w_down, const void* gate_up, Act act,
                                    void* dgate_up, hipStream_t s) {
     return by_act(act, [&](auto a) {
@@ -217,7 +304,7 @@ cobalt_status launch_down_gradient(const Groups& g, const void* dout, Rows rows,
     });
 }
 
-cobalt_status launch_gate_up_gradient(const Groups& g, const void* dgate_up, int64_t d, int64_t f,
+static cobalt_status launch_gate_up_gradient(const Groups& g, const void* dgate_up, int64_t d, int64_t f,
                                       const void* w_in, Rows rows, void* dx, hipStream_t s) {
     return by_bool(f % 32 == 0, [&](auto whole) {
         return by_shape<Along::kOne>(g, d, tiles(2 * f, 64), [&](auto shape) {
@@ -233,7 +320,9 @@ cobalt_status launch_gate_up_gradient(const Groups& g, const void* dgate_up, int
     });
 }
 
-cobalt_status launch_weight_gradient(const Groups& g, const void* a, int64_t na, bool a_rows,
+// dw[e] (+)= sum_i a[i] b[i]^T over the places of e: a [.][na], b [.][nb], the
+// one taken at place i, the other at its row (a_rows: a).
+static cobalt_status launch_weight_gradient(const Groups& g, const void* a, int64_t na, bool a_rows,
                                      const void* b, int64_t nb, Rows rows, void* dw,
                                      bool f32, bool add, void* ws, hipStream_t s) {
     const auto run = [&](auto shape, auto in_float, auto in_add, auto ga, auto gb, int parts,
@@ -279,6 +368,55 @@ cobalt_status launch_weight_gradient(const Groups& g, const void* a, int64_t na,
             return g.E * tiles(na, S::kBM) * tiles(nb, S::kBN);
         },
         by_type);
+}
+
+cobalt_status launch_down_backward(const Groups& g, const void* dout, Rows rows, int64_t d,
+                                   int64_t f, const void* w_down, const void* gate_up,
+                                   const void* h, Act act, void* dgate_up, void* dw, bool f32,
+                                   bool add, void* ws, hipStream_t s) {
+    const bool some = g.M > 0 && dgate_up;
+    if (const Both b = together(g, f, d, f); some && dw && b.ok)
+        return by_act(act, [&](auto a) {
+            return by_bool(d % 64 == 0, [&](auto whole) {
+                return by_result(f32, add, rows.idx, [&](auto in_float, auto in_add, auto of) {
+                    down_backward_kernel<a(), whole(), in_float(), in_add(), of()>
+                        <<<b.all + b.all_w, Small::kThreads, 0, s>>>(
+                            g, b.all, b.all_w, b.mt, (const char*)dout, rows, d, f,
+                            (const char*)w_down, (const uint16_t*)gate_up, (uint16_t*)dgate_up,
+                            (const char*)h, dw);
+                    COBALT_LAUNCH_CHECK();
+                    return COBALT_OK;
+                });
+            });
+        });
+    if (dw)
+        if (cobalt_status st = launch_weight_gradient(g, dout, d, true, h, f, rows, dw, f32, add,
+                                                      ws, s))
+            return st;
+    return some ? launch_down_gradient(g, dout, rows, d, f, w_down, gate_up, act, dgate_up, s)
+                : COBALT_OK;
+}
+
+cobalt_status launch_gate_up_backward(const Groups& g, const void* dgate_up, const void* x,
+                                      Rows rows, int64_t d, int64_t f, const void* w_in, void* dx,
+                                      void* dw, bool f32, bool add, void* ws, hipStream_t s) {
+    const bool some = g.M > 0 && rows.n > 0 && dx;
+    if (const Both b = together(g, d, 2 * f, d); some && dw && b.ok)
+        return by_bool(f % 32 == 0, [&](auto whole) {
+            return by_result(f32, add, rows.idx, [&](auto in_float, auto in_add, auto of) {
+                gate_up_backward_kernel<whole(), in_float(), in_add(), of()>
+                    <<<b.all + b.all_w, Small::kThreads, 0, s>>>(
+                        g, b.all, b.all_w, b.mt, (const char*)dgate_up, d, f, (const char*)w_in,
+                        rows, (uint16_t*)dx, (const char*)x, dw);
+                COBALT_LAUNCH_CHECK();
+                return COBALT_OK;
+            });
+        });
+    if (dw)
+        if (cobalt_status st = launch_weight_gradient(g, dgate_up, 2 * f, false, x, d, rows, dw,
+                                                      f32, add, ws, s))
+            return st;
+    return some ? launch_gate_up_gradient(g, dgate_up, d, f, w_in, rows, dx, s) : COBALT_OK;
 }
 
 size_t expert_backward_workspace_bytes(int64_t M, int E, int64_t d, int64_t f) {

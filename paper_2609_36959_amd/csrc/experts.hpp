@@ -129,16 +129,14 @@ cobalt_status launch_gate_up(const Groups& g, const void* x, Rows rows, int64_t 
                              const void* w_in, Act act, void* h, void* gate_up, hipStream_t s);
 cobalt_status launch_down(const Groups& g, const void* h, int64_t d, int64_t f,
                           const void* w_down, Rows rows, void* out, hipStream_t s);
-cobalt_status launch_down_gradient(const Groups& g, const void* dout, Rows rows, int64_t d,
-                                   int64_t f, const void* w_down, const void* gate_up, Act act,
-                                   void* dgate_up, hipStream_t s);
-cobalt_status launch_gate_up_gradient(const Groups& g, const void* dgate_up, int64_t d, int64_t f,
-                                      const void* w_in, Rows rows, void* dx, hipStream_t s);
-// dw[e] (+)= sum_i a[i] b[i]^T over the places of e: a [.][na], b [.][nb], the
-// one taken at place i, the other at its row (a_rows: a).
-cobalt_status launch_weight_gradient(const Groups& g, const void* a, int64_t na, bool a_rows,
-                                     const void* b, int64_t nb, Rows rows, void* dw,
-                                     bool f32, bool add, void* ws, hipStream_t s);
+// Either result may be NULL.
+cobalt_status launch_down_backward(const Groups& g, const void* dout, Rows rows, int64_t d,
+                                   int64_t f, const void* w_down, const void* gate_up,
+                                   const void* h, Act act, void* dgate_up, void* dw, bool f32,
+                                   bool add, void* ws, hipStream_t s);
+cobalt_status launch_gate_up_backward(const Groups& g, const void* dgate_up, const void* x,
+                                      Rows rows, int64_t d, int64_t f, const void* w_in, void* dx,
+                                      void* dw, bool f32, bool add, void* ws, hipStream_t s);
 size_t expert_backward_workspace_bytes(int64_t M, int E, int64_t d, int64_t f);
 
 cobalt_status launch_mx_quantize(const void* x, int64_t R, int64_t n, void* codes, void* scales,
