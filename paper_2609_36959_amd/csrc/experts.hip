@@ -4,10 +4,11 @@
 // In the first two the weights' rows are k, and in the last both operands'
 // places are: such operands lie across k in memory and are turned on their way
 // out of LDS. All are bound by the matrix cores, as the forward products are.
-// 16384 rows of 8 experts, 7168 x 2048 | 24576 of 64, 2048 x 1024 | 1018 of 16,
-// 512 x 256, in us: dgate_up 567 | 220 | 13, dx 963 | 342 | 10, dw_down 597 |
-// 216 | 6.5, dw_in 1085 | 403 | 7 (0.85, 0.60; 1.00, 0.60; 0.81, 0.48; 0.89,
-// 0.51 PFLOP/s of the first two, whose experts' uneven rows leave tiles short).
+// 16384 rows of 8 experts, 7168 x 2048 | 24576 of 64, 2048 x 1024, in us:
+// dgate_up 567 | 220, dx 963 | 342, dw_down 597 | 216, dw_in 1085 | 403 (0.85,
+// 0.47; 1.00, 0.60; 0.81, 0.48; 0.89, 0.51 PFLOP/s: experts' uneven rows leave
+// tiles short). 1018 rows of 16 experts of 512 x 256 are bound by latency: 14
+// and 11 us for the two calls, each with both its gradients in one launch.
 #include "few.hpp"
 
 namespace cobalt {
@@ -180,8 +181,8 @@ __global__ __launch_bounds__(S::kThreads, 2) void weight_gradient_kernel(
 }
 
 // The rows' gradients and the weights' of a call in one launch, workgroups
-// [0, all) and [all, all + all_w): neither reads what the other writes. For
-// small calls, whose launches leave CUs idle one after the other (together()).
+// [0, all) and [all, all + all_w): neither reads what the other writes. together() says
+// when.
 typedef Shape<2, 2> Small;
 template <Act A, bool kWhole, bool kFloat, bool kAdd, bool kGather>
 __global__ __launch_bounds__(Small::kThreads, 2) void down_backward_kernel(
@@ -235,7 +236,10 @@ int parts_of(int64_t M, int E, int64_t na, int64_t nb) {
 }
 
 // The launch of a call's gradients of rows, of n columns, and of na x nb weights
-// in one kernel, if all their tiles are expected to be on the CUs at once.
+// in one kernel, with the smallest tiles for both: while they are expected to be
+// few, as the two launches then wait for each other's last tiles. In one launch |
+// in two, us by the number of tiles: 522 14 | 29, 776 20 | 36, 1304 21 | 34,
+// 2328 33 | 52, 4656 57 | 65, 6224 101 | 89.
 struct Both {
     uint32_t all = 0, all_w = 0, mt = 0;
     bool ok = false;
@@ -243,7 +247,7 @@ struct Both {
 Both together(const Groups& g, int64_t n, int64_t na, int64_t nb) {
     constexpr int kBM = Small::kBM, kBN = Small::kBN;
     Both b;
-    if (expected_tiles(g, kBM) * tiles(n, kBN) + g.E * tiles(na, kBM) * tiles(nb, kBN) > 3 * 256 ||
+    if (expected_tiles(g, kBM) * tiles(n, kBN) + g.E * tiles(na, kBM) * tiles(nb, kBN) > 20 * 256 ||
         parts_of(g.M, g.E, na, nb) > 1)
         return b;
     const int64_t all = tile_grid(most_tiles(g.M, g.E, kBM), tiles(n, kBN)),
