@@ -378,7 +378,8 @@ cobalt_status cobalt_expert_down(const void* h, const int32_t* expert_offsets, i
 
 /* Workspace of the two calls below (partial weight gradients of experts
  * whose rows are split), 256-byte aligned, owned by the caller, contents
- * ignored, not shared by calls that may overlap. */
+ * ignored, not shared by calls that may overlap. The size does not fall as M
+ * grows. */
 size_t cobalt_expert_backward_workspace_bytes(int64_t M, int32_t E, int64_t d, int64_t f);
 
 /* Gradients of the output projection, the product and the activation. With

@@ -140,3 +140,10 @@ def test_backward_workspace():
     size = B.cobalt_expert_backward_workspace_bytes
     assert size(8, 4, 16, 16) >= 256
     assert size(-1, 4, 16, 16) == size(8, 0, 16, 16) == size(8, 4, 12, 16) == size(8, 4, 16, 0) == 0
+
+
+def test_backward_workspace_grows_with_places():
+    size = B.cobalt_expert_backward_workspace_bytes
+    for E, d, f in ((1, 64, 32), (4, 512, 256), (8, 1024, 512), (64, 2048, 1024)):
+        sizes = [size(M, E, d, f) for M in (0, 1, 500, 4096, 5000, 16384, 100000, 2**31 - 512)]
+        assert sizes == sorted(sizes) and sizes[0] == 256
